@@ -1,7 +1,9 @@
 /*
  * libswitchback -- the SwitchBack int8 linear layer (arxiv 2304.13013, Section 2.2.1, Algorithm 1) for one
  * AMD MI355X (gfx950), as a C ABI.  Declared after the five calls of Algorithm 1: the layer's variants from the same
- * paper (SwitchBackM, SwitchBackQ, float8) and its optimizer (StableAdamW), each with the passage it follows.
+ * paper (SwitchBackM, SwitchBackQ, float8) and its optimizer (StableAdamW), each with the passage it follows, and what a
+ * transformer block has next to them: the float8 layer with a scale for each block of 128, also with a weight per expert,
+ * and layer norm with its gradients.
  *
  * Notation (Section 2.2.1 "Notation"): X [b,n] inputs, W [m,n] weights (an nn.Linear weight, out x in),
  * Y = X W^T [b,m]; dY [b,m] the gradient of the loss w.r.t. Y, dX = dY W [b,n], dW = dY^T X [m,n];
@@ -52,7 +54,9 @@ typedef enum {
     SB_OP_BACKWARD_INPUT = 2,
     SB_OP_BACKWARD_WEIGHT = 3,
     SB_OP_QUANTIZE_COLWISE = 4, /* also the workspace of switchback_backward_input_q; pass rows as m, cols as n */
-    SB_OP_STABLE_ADAMW = 5      /* shape arguments ignored */
+    SB_OP_STABLE_ADAMW = 5,     /* shape arguments ignored */
+    SB_OP_LAYER_NORM_BACKWARD = 6, /* pass rows as b, cols as n */
+    SB_OP_LINEAR_F8_BLOCK = 7   /* pass the layer's input width as n; m ignored */
 } sb_op;
 
 /* What the forward pass leaves for the backward pass (Algorithm 1 saves X and W in 16 bit and re-quantizes W in
@@ -217,6 +221,76 @@ int switchback_forward_f8(const void *x_bf16, const void *w_bf16, int64_t b, int
 int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int64_t b, int64_t n, int64_t m, void *dx,
                                  sb_dtype dx_dtype, uint8_t *gq, float *state_g, sb_f8_format fmt_g,
                                  sb_f8_format fmt_w, void *stream);
+
+/* The float8 layer with a scale for each block of 128, plain and grouped by expert.  Where the float8 variant above has one
+ * state per row and one for the whole weight, here every 128 values have a scale of their own: X and dY in blocks of 1 x 128
+ * along their rows, W in blocks of 128 x 128 (the last ones of a row or column may be shorter).  Scales are powers of two,
+ *   e = the least integer >= -127 with absmax(block) <= MAX * 2^e   (MAX = 448 for SB_E4M3, 57344 for SB_E5M2),
+ *   code = float8cast(x * 2^-e), round to nearest even;   scale byte = e + 127;   the block stands for value(code) * 2^e,
+ * so that nothing but the cast rounds, and Q(W^T) = Q(W)^T with the same scales.  A block without a nonzero value has scale
+ * byte 0.  Scale bytes are 0 .. 247.
+ *
+ * Layouts.  Code rows are whole blocks: K = the row's length rounded up to a multiple of 128, zero codes behind its end.
+ * Row scales: [rows, S] bytes with S = K / 128 rounded up to a multiple of 4, 0 behind the last block.  Weight scales:
+ * [ceil(m / 128), K / 128] bytes.  All are 16-byte aligned.
+ *
+ * Experts.  With offsets == NULL there is one weight (experts == 1) and it goes with all rows.  Otherwise weights, codes,
+ * scales and weight gradients are [experts, ...] and `offsets` is a device array of experts + 1 non-decreasing int32 row
+ * numbers: rows offsets[e] .. offsets[e+1] - 1 of X, Y, dX and dY are expert e's (none if the two are equal).  Rows before
+ * offsets[0] and from offsets[experts] on belong to no expert: their outputs are left as they were.  Offsets are read when the
+ * call's kernels run, not on the host, and clamped to 0 .. b: others than documented give unspecified values, never a fault.
+ * 1 <= experts <= 1024.
+ *
+ * switchback_quantize_rowwise_f8_block: x [rows,cols] bf16 -> codes [rows,K], scales [rows,S].  cols % 8 == 0, cols <= 131072.
+ * switchback_quantize_weight_f8_block: w [experts,m,n] bf16 -> codes [experts,m,K(n)], scales [experts,ceil(m/128),K(n)/128]
+ *   and, unless NULL, the transpose: codes_t [experts,n,K(m)], scales_t [experts,ceil(n/128),K(m)/128].  m % 64 == 0,
+ *   n % 64 == 0.
+ * switchback_matmul_f8_block: out[i,j] = sum_kb 2^(ea[i,kb] + eb[j/128,kb]) sum_{k in kb} value(aq[i,k]) value(bq[e,j,k]), e the
+ *   expert of row i; binary32 accumulation (order unspecified but deterministic; it may depend on the row's place, and the
+ *   matrix instruction drops what lies 2^13 below the largest of eight neighbouring products), rounded to nearest even
+ *   when SB_BF16.  aq [M,K], scales_a [M,S], bq [experts,N,K], scales_b [experts,ceil(N/128),K/128]; out [M,N], SB_BF16 or
+ *   SB_F32.  K % 128 == 0, N % 64 == 0, K, N <= 131072, (M + 256) * max(K, N) * 2 < 2^32, (N + 256) * K < 2^32.
+ * switchback_linear_f8_block: X [b,n] bf16 quantized by rows in fmt_x, then the product with a weight's codes wq [experts,m,K]
+ *   in fmt_w, scales_w: the layer with codes that are kept (serving), and with (dY, codes_t, scales_t, n = m, m = n) its input
+ *   gradient.  y [b,m].  ws: SB_OP_LINEAR_F8_BLOCK workspace.
+ * switchback_forward_f8_block: W [experts,m,n] quantized (into the four code and scale arrays, codes_t and scales_t may be
+ *   NULL), then as switchback_linear_f8_block.  b == 0 still quantizes W.  m % 64 == 0, n % 64 == 0; other limits as above.
+ * The weight gradient of the plain layer is switchback_backward_weight, with experts switchback_backward_weight_experts: dW[e]
+ *   = dY^T X over the rows of expert e, 16-bit operands, binary32 accumulation; zeros for an expert without rows.  dw
+ *   [experts,m,n], SB_BF16 or SB_F32; ws: switchback_backward_weight_experts_workspace_bytes(b, n, m, experts) bytes. */
+int switchback_quantize_rowwise_f8_block(const void *x_bf16, int64_t rows, int64_t cols, sb_f8_format fmt, uint8_t *codes,
+                                         uint8_t *scales, void *stream);
+int switchback_quantize_weight_f8_block(const void *w_bf16, int64_t experts, int64_t m, int64_t n, sb_f8_format fmt,
+                                        uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, void *stream);
+int switchback_matmul_f8_block(const uint8_t *aq, sb_f8_format fmt_a, const uint8_t *scales_a, const uint8_t *bq,
+                               sb_f8_format fmt_b, const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M,
+                               int64_t N, int64_t K, void *out, sb_dtype out_dtype, void *stream);
+int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint8_t *scales_w, const int32_t *offsets,
+                               int64_t experts, int64_t b, int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, void *y,
+                               sb_dtype y_dtype, void *ws, size_t ws_bytes, void *stream);
+int switchback_forward_f8_block(const void *x_bf16, const void *w_bf16, const int32_t *offsets, int64_t experts, int64_t b,
+                                int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, uint8_t *wq, uint8_t *scales_w,
+                                uint8_t *wq_t, uint8_t *scales_wt, void *y, sb_dtype y_dtype, void *ws, size_t ws_bytes,
+                                void *stream);
+int switchback_backward_weight_experts(const void *dy_bf16, const void *x_bf16, const int32_t *offsets, int64_t experts,
+                                       int64_t b, int64_t n, int64_t m, void *dw, sb_dtype dw_dtype, void *ws, size_t ws_bytes,
+                                       void *stream);
+size_t switchback_backward_weight_experts_workspace_bytes(int64_t b, int64_t n, int64_t m, int64_t experts);
+
+/* Layer norm over the rows of x [rows,cols] (SB_BF16 or SB_F32, `dtype`), the operation in front of a transformer block's
+ * linear layers, with its gradients.  mu and r = 1 / sqrt(var + eps) per row (var the mean of the squared differences from
+ * mu), h = (x - mu) * r, y = h * gamma + beta; binary32 arithmetic, y rounded once.
+ *   y [rows,cols] in dtype; gamma, beta [cols] f32 or NULL (1 and 0); mean, rstd [rows] f32 or NULL; eps > 0.
+ * Backward, with a = dy * gamma:  dx = r * (a - mean_j(a) - h * mean_j(a * h)),  dgamma = sum_i dy * h,  dbeta = sum_i dy.
+ *   dy, dx [rows,cols] in dtype; mean, rstd as the forward pass left them; gamma [cols] f32 or NULL; dgamma, dbeta [cols] f32,
+ *   either or both NULL; their sums are formed in a fixed order (deterministic; no rows give zeros).
+ *   ws: SB_OP_LAYER_NORM_BACKWARD workspace (not needed if dgamma and dbeta are NULL).
+ * 1 <= cols <= 65536, rows <= 2^30; matrices, gamma and beta 16-byte aligned (dgamma, dbeta, mean, rstd 4-byte). */
+int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, const float *beta, float eps, int64_t rows,
+                          int64_t cols, void *y, float *mean, float *rstd, void *stream);
+int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype, const float *mean, const float *rstd,
+                                   const float *gamma, int64_t rows, int64_t cols, void *dx, float *dgamma, float *dbeta,
+                                   void *ws, size_t ws_bytes, void *stream);
 
 /* One StableAdamW step for one parameter tensor (the optimizer algorithm of the paper's section on loss spikes: AdamW
  * with the debiasing folded into the decay rates and update clipping; the implementation note of the appendix gives

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswitchback.so")
 BINDING = os.path.join(HERE, "_binding" + sysconfig.get_config_var("EXT_SUFFIX"))  # of this Python alone
 SOURCES = ["quantize.hip", "gemm_i8.hip", "gemm_i8_direct.hip", "gemm_f8.hip", "gemm_bf16_tn.hip", "stable_adamw.hip", "switchback_api.hip",
-           "ceilings.hip"]
+           "ceilings.hip", "quantize_block.hip", "gemm_f8_block.hip", "layer_norm.hip"]
 
 # -ffp-contract=off: the quantizers and the dequantizing epilogue promise one rounding per operation.
 # The packed-fp32 feature is switched off on purpose (plain v_mul/v_add/v_fma only).

@@ -71,7 +71,7 @@ PyObject *dev(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
 
 // out(t, shape, dtype, device, name): a fresh output tensor, or the caller's if it has exactly this shape and type.
 PyObject *out(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
-    constexpr Py_ssize_t MAX_RANK = 2;
+    constexpr Py_ssize_t MAX_RANK = 3;
     if (nargs == 5 && PyTuple_CheckExact(args[1]) && PyTuple_GET_SIZE(args[1]) <= MAX_RANK && THPDtype_Check(args[2]) &&
         THPDevice_Check(args[3])) {
         int64_t shape[MAX_RANK];
@@ -189,7 +189,15 @@ PyMethodDef bound_methods[] = {SB_METHOD("dev", &dev),
                                SB_ENTRY(matmul_f8_dequant),
                                SB_ENTRY(forward_f8),
                                SB_ENTRY(backward_input_f8),
-                               SB_ENTRY(stable_adamw_step_multi)};
+                               SB_ENTRY(stable_adamw_step_multi),
+                               SB_ENTRY(quantize_rowwise_f8_block),
+                               SB_ENTRY(quantize_weight_f8_block),
+                               SB_ENTRY(matmul_f8_block),
+                               SB_ENTRY(linear_f8_block),
+                               SB_ENTRY(forward_f8_block),
+                               SB_ENTRY(backward_weight_experts),
+                               SB_ENTRY(layer_norm),
+                               SB_ENTRY(layer_norm_backward)};
 constexpr size_t ENTRIES = sizeof(bound_methods) / sizeof(bound_methods[0]) - CHECKS;
 
 // bind(dev, out, saved_type, entry) -> {name: built-in function}: the general forms of the checks, the ctypes structure of

@@ -26,6 +26,16 @@ __global__ __launch_bounds__(Small::THREADS) __attribute__((amdgpu_waves_per_eu(
     gemm_bf16_tn_body<true>(p);
 }
 
+// A gradient per expert.
+__global__ __launch_bounds__(Big::THREADS) __attribute__((amdgpu_waves_per_eu(1, 1))) void gemm_bf16_tn_experts_kernel(
+    GemmBf16ExpertArgs p) {
+    gemm_bf16_tn_wide_body(p);
+}
+__global__ __launch_bounds__(Small::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void gemm_bf16_tn_experts_small_kernel(
+    GemmBf16ExpertArgs p) {
+    gemm_bf16_tn_body<false>(p);
+}
+
 // out[e] = sum over splits (ascending) of partial[s][e]; four elements per thread, eight splits' loads in flight.
 __global__ __launch_bounds__(256) void splitk_reduce_kernel(const v4f *__restrict__ partial, int64_t quads,
                                                             int splits, void *__restrict__ out, int out_bf16) {
@@ -47,8 +57,8 @@ __global__ __launch_bounds__(256) void splitk_reduce_kernel(const v4f *__restric
         static_cast<v4f *>(out)[i] = s;
 }
 
-template <class C>
-hipError_t set_lds_limit_once(void (*kernel)(GemmBf16Args), std::atomic<bool> &done) {
+template <class C, class Args>
+hipError_t set_lds_limit_once(void (*kernel)(Args), std::atomic<bool> &done) {
     if (done.load(std::memory_order_acquire)) return hipSuccess;  // a second set by a racing host thread is harmless
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES);
@@ -105,6 +115,56 @@ hipError_t launch_gemm_bf16_tn(const WeightGradPlan &plan, const void *dy, const
     const int64_t quads = m * n / 4;
     splitk_reduce_kernel<<<(unsigned int)((quads + 255) / 256), 256, 0, stream>>>(
         static_cast<const v4f *>(ws), quads, a.splits, dw, a.out_bf16);
+    return hipGetLastError();
+}
+
+// Which tiles, and how many splits of an expert's tokens: at most 16, and 256 tokens each in the mean, until there is an item for
+// every slot.
+ExpertGradPlan plan_gemm_bf16_tn_experts(int64_t b, int64_t n, int64_t m, int64_t experts) {
+    ExpertGradPlan plan{true, 1};
+    const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * experts;
+    while (plan.splits < 16 && tiles * plan.splits < num_compute_units() && b / (experts * plan.splits * 2) >= 256) plan.splits *= 2;
+    return plan;
+}
+
+size_t gemm_bf16_tn_experts_workspace_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts) {
+    return plan.splits > 1 ? (size_t)plan.splits * (size_t)experts * (size_t)m * (size_t)n * sizeof(float) : 0;
+}
+
+hipError_t launch_gemm_bf16_tn_experts(const ExpertGradPlan &plan, const void *dy, const void *x, const int32_t *offsets, int64_t experts,
+                                       int64_t b, int64_t n, int64_t m, void *dw, sb_dtype dw_dtype, void *ws, hipStream_t stream) {
+    static std::atomic<bool> big_set{false}, small_set{false};
+    hipError_t e = plan.small ? set_lds_limit_once<Small>(gemm_bf16_tn_experts_small_kernel, small_set)
+                              : set_lds_limit_once<Big>(gemm_bf16_tn_experts_kernel, big_set);
+    if (e != hipSuccess) return e;
+    GemmBf16ExpertArgs a;
+    a.dy = static_cast<const unsigned short *>(dy);
+    a.x = static_cast<const unsigned short *>(x);
+    a.b = (int)b;
+    a.n = (int)n;
+    a.m = (int)m;
+    const int side = plan.small ? 128 : 256;
+    a.tiles_m = (int)((m + side - 1) / side);
+    a.tiles_n = (int)((n + side - 1) / side);
+    a.splits = plan.splits;
+    a.k_per_split = a.k_per_piece = 0;
+    a.partial = static_cast<float *>(ws);
+    a.out = dw;
+    a.out_bf16 = dw_dtype == SB_BF16;
+    a.offsets = offsets;
+    a.experts = (int)experts;
+    // A workgroup per item: experts differ in length, and a compute unit that is done takes the next one.
+    const int64_t total = (int64_t)a.tiles_m * a.tiles_n * a.splits * experts;
+    const int grid = (int)((total + 7) / 8 * 8);
+    if (plan.small)
+        gemm_bf16_tn_experts_small_kernel<<<grid, Small::THREADS, Small::LDS_BYTES, stream>>>(a);
+    else
+        gemm_bf16_tn_experts_kernel<<<grid, Big::THREADS, Big::LDS_BYTES, stream>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int64_t quads = experts * m * n / 4;
+    splitk_reduce_kernel<<<(unsigned int)((quads + 255) / 256), 256, 0, stream>>>(static_cast<const v4f *>(ws), quads, a.splits, dw,
+                                                                                   a.out_bf16);
     return hipGetLastError();
 }
 

@@ -36,6 +36,26 @@ struct GemmBf16Args {
     int k_per_piece;  // FOLD instances only (splits == 1): tokens per partial sum, a multiple of the stage length
 };
 
+// A gradient per expert: dW[e] is the sum over the tokens offsets[e] .. offsets[e + 1] - 1, out [experts,m,n], partial
+// [splits][experts][m][n].  The instances for these arguments are kernels of their own.
+struct GemmBf16ExpertArgs : GemmBf16Args {
+    const int *offsets;  // [experts + 1]
+    int experts;
+};
+
+// The tokens of one split of an expert's range, clamped to what there is; a split is whole stages of the range.
+struct ExpertTokens {
+    int first, end;  // of the split
+};
+__device__ __forceinline__ ExpertTokens expert_tokens(const GemmBf16ExpertArgs &p, int expert, int split, int stage) {
+    const int first = min(max(p.offsets[expert], 0), p.b), end = min(max(p.offsets[expert + 1], first), p.b);
+    const int per = ((end - first + p.splits - 1) / p.splits + stage - 1) / stage * stage;
+    ExpertTokens t;
+    t.first = __builtin_amdgcn_readfirstlane(min(first + split * per, end));
+    t.end = __builtin_amdgcn_readfirstlane(min(t.first + per, end));
+    return t;
+}
+
 // 80 KiB of LDS, so two workgroups share a compute unit; all four waves load.
 struct GemmBf16Cfg {
     static constexpr int BM = 128, BN = 128, BKT = 64;        // dW rows (dY columns), dW columns (X columns), tokens/stage
@@ -57,10 +77,12 @@ struct GemmBf16Cfg {
 
 // FOLD: the token range is one item, but its pieces of k_per_piece tokens are summed on their own and added in token
 // order, in registers: the bits of the split product and its reduction, without the second launch.
+// With GemmBf16ExpertArgs an expert without tokens gets zeros.
 // (A __device__ function: a __global__ template that uses device-only buffer builtins does not instantiate in the host
 // pass; the __global__ entries live next to the launcher.)
-template <bool FOLD>
-__device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
+template <bool FOLD, class Args>
+__device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
+    constexpr bool EXPERTS = std::is_same<Args, GemmBf16ExpertArgs>::value;
     typedef GemmBf16Cfg C;
     constexpr int MT = C::MT;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // wave-uniform: what derives from it is scalar
@@ -84,7 +106,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
     const bool loads_dy = wave * C::LPW < C::REQ_OP;
     const unsigned ld = loads_dy ? p.m : p.n;  // row length of the operand this wave loads
     // The bounds check of the buffer resource (num_records in bytes) turns token rows past b into zeros.
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+    __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
         (void *)(loads_dy ? p.dy : p.x), 0, (unsigned)((size_t)p.b * ld * 2), 0x00020000);
     const int l_tok = lane / C::CHUNKS, l_pos = lane % C::CHUNKS;  // token row of the request, 16-byte chunk of it
     const int tok0 = ((wave * C::LPW) % C::REQ_OP) * C::ROWS_PER_REQ;  // first token row of the wave's share within a stage
@@ -171,8 +193,11 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
     // [r * grid, (r + 1) * grid), and XCD x (workgroup id % 8) the x-th run of grid / 8 consecutive items of it: the
     // workgroups sharing an L2 read one token range and neighbouring tiles, and all XCDs stream the same few token
     // ranges at the same time, so what one fetched from HBM the others find in the last-level cache.
-    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits;
+    const int tiles = p.tiles_m * p.tiles_n;
+    int total = tiles * p.splits;
+    if constexpr (EXPERTS) total *= p.experts;
     const int xcd = blockIdx.x & 7, slots = gridDim.x >> 3;
+    // (EXPERTS: the splits of an expert follow each other, `split` is expert * splits + split.)
     auto item_of = [&](int round, int *tm, int *tn, int *split) -> bool {
         const int item = round * (int)gridDim.x + xcd * slots + (blockIdx.x >> 3);
         if (item >= total) return false;
@@ -188,8 +213,21 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
         return true;
     };
     auto stages_of = [&](int split) -> int {
+        if constexpr (EXPERTS) {
+            const ExpertTokens t = expert_tokens(p, split / p.splits, split % p.splits, C::BKT);
+            return (t.end - t.first + C::BKT - 1) / C::BKT;
+        }
         const int k_begin = split * p.k_per_split, k_end = min(p.b, k_begin + p.k_per_split);
         return k_end > k_begin ? (k_end - k_begin + C::BKT - 1) / C::BKT : 0;
+    };
+
+    auto token_of = [&](int split) -> int {  // first token; EXPERTS: those from the end of the expert's on are to read as zero
+        if constexpr (EXPERTS) {
+            const ExpertTokens t = expert_tokens(p, split / p.splits, split % p.splits, C::BKT);
+            rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(loads_dy ? p.dy : p.x), 0, (unsigned)((size_t)t.end * ld * 2), 0x00020000);
+            return t.first;
+        }
+        return split * p.k_per_split;
     };
 
     int tm, tn, split;
@@ -197,7 +235,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
     int KT = 0;
     if (have) {
         KT = stages_of(split);
-        set_item_sources(tm, tn, split * p.k_per_split);
+        set_item_sources(tm, tn, token_of(split));
 #pragma unroll
         for (int s = 0; s < S; ++s)
             if (s < KT) issue_stage(s);
@@ -297,7 +335,10 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
         }
 
         const int m_base = tm * C::BM + wm0, n_base = tn * C::BN + wn0;
-        const int this_split = split;
+        // Matrices before this item's in the output, or in the partial sums.
+        const int out_matrix = EXPERTS ? split / p.splits : 0;
+        int this_split = split;
+        if constexpr (EXPERTS) this_split = split % p.splits * p.experts + split / p.splits;
 
         // Every wave is done reading the stages: request the next item's stages, then store this item's results.
         wait_lds_reads();
@@ -307,7 +348,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
         int nKT = 0;
         if (have) {
             nKT = stages_of(nsplit);
-            set_item_sources(ntm, ntn, nsplit * p.k_per_split);
+            set_item_sources(ntm, ntn, token_of(nsplit));
 #pragma unroll
             for (int s = 0; s < S; ++s)
                 if (s < nKT) issue_stage(s);
@@ -315,7 +356,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
 
         if (p.splits == 1 && p.out_bf16) {
             // Final bf16 result: transpose through the wave-private LDS patch, 16-byte stores in 128-byte row segments.
-            unsigned short *out = static_cast<unsigned short *>(p.out);
+            unsigned short *out = static_cast<unsigned short *>(p.out) + (EXPERTS ? (int64_t)out_matrix * p.m * p.n : 0);
             unsigned char *epi = smem + S * C::STAGE_BYTES + wave * C::EPI_WAVE_BYTES;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -342,7 +383,8 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const GemmBf16Args &p) {
             }
         } else {
             // binary32: final result (one split) or this split's partial sums, straight from the registers.
-            float *pout = p.splits > 1 ? p.partial + (int64_t)this_split * p.m * p.n : static_cast<float *>(p.out);
+            float *pout = p.splits > 1 ? p.partial + (int64_t)this_split * p.m * p.n
+                                       : static_cast<float *>(p.out) + (EXPERTS ? (int64_t)out_matrix * p.m * p.n : 0);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll

@@ -40,8 +40,11 @@ struct WideCfg {
     static_assert((STAGES & (STAGES - 1)) == 0 && LDS_BYTES <= 160 * 1024, "configuration");
 };
 
-// No item may be empty (every token range holds a token): the caller sees to it.
-__device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
+// No item may be empty (every token range holds a token): the caller sees to it.  With GemmBf16ExpertArgs the empty ranges are a
+// pair of stages of zeros.
+template <class Args>
+__device__ __forceinline__ void gemm_bf16_tn_wide_body(const Args &p) {
+    constexpr bool EXPERTS = std::is_same<Args, GemmBf16ExpertArgs>::value;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     typedef __attribute__((address_space(3))) void lds_void;
     typedef WideCfg C;
@@ -66,11 +69,14 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
     const unsigned req_step = 4 * ld, stage_step = (unsigned)C::BKT * 2 * ld;
 
     // Work items (GemmBf16Args): this workgroup's item `round` counts if it is below `total`.
-    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits;
+    const int tiles = p.tiles_m * p.tiles_n;
+    int total = tiles * p.splits;
+    if constexpr (EXPERTS) total *= p.experts;
     const int first = (blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
     struct Item {
         int tm, tn, split, stages;  // stages: even
         bool have;
+        int token, end, matrix;  // EXPERTS: first token, the tokens from `end` on read as zero, the expert
     };
     auto item_of = [&](int round) -> Item {
         const int id = round * (int)gridDim.x + first;
@@ -81,7 +87,19 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
         const int i = tile % minor, j = tile / minor;
         it.tm = p.tiles_m < p.tiles_n ? i : j;
         it.tn = p.tiles_m < p.tiles_n ? j : i;
-        it.stages = (min(p.b - it.split * p.k_per_split, p.k_per_split) + C::UNIT - 1) / C::UNIT * 2;
+        if constexpr (EXPERTS) {
+            it.token = it.end = it.matrix = it.stages = 0;
+            if (it.have) {
+                it.matrix = it.split / p.splits;
+                it.split = it.split % p.splits;
+                const ExpertTokens t = expert_tokens(p, it.matrix, it.split, C::UNIT);
+                it.token = t.first;
+                it.end = t.end;
+                it.stages = max((t.end - t.first + C::UNIT - 1) / C::UNIT, 1) * 2;
+            }
+        } else {
+            it.stages = (min(p.b - it.split * p.k_per_split, p.k_per_split) + C::UNIT - 1) / C::UNIT * 2;
+        }
         return it;
     };
 
@@ -91,8 +109,8 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
     auto next_item_sources = [&]() {
         const Item it = item_of(l_round++);
         l_left = it.have ? it.stages : 1 << 30;
-        l_bytes = it.have ? (unsigned)p.b * ld * 2 : 0;
-        l_soff = ((unsigned)(it.split * p.k_per_split + tok0) * ld + (unsigned)(loads_dy ? it.tm * C::BM : it.tn * C::BN)) * 2;
+        l_bytes = it.have ? (unsigned)(EXPERTS ? it.end : p.b) * ld * 2 : 0;
+        l_soff = ((unsigned)((EXPERTS ? it.token : it.split * p.k_per_split) + tok0) * ld + (unsigned)(loads_dy ? it.tm * C::BM : it.tn * C::BN)) * 2;
     };
     auto issue_req = [&](int slot, int i) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -218,7 +236,8 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
         if (p.splits == 1 && p.out_bf16) {
             // Final bf16 result: transposed through the wave-private patch, 256-byte row segments.
             const __amdgpu_buffer_rsrc_t rsrc_out = __builtin_amdgcn_make_buffer_rsrc(
-                static_cast<unsigned short *>(p.out) + (int64_t)m_base * n + n_base, 0, rows_in * n * 2, 0x00020000);
+                static_cast<unsigned short *>(p.out) + (EXPERTS ? (int64_t)it.matrix * p.m * n : 0) + (int64_t)m_base * n + n_base, 0,
+                rows_in * n * 2, 0x00020000);
             unsigned char *epi = smem + S * C::STAGE_BYTES + wave * C::EPI_WAVE_BYTES;
             const unsigned o_voff = e_r * 8 < cols_in ? (unsigned)(e_g * n + e_r * 8) * 2 : NOWHERE;
 #pragma unroll
@@ -244,7 +263,10 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const GemmBf16Args &p) {
             }
         } else {
             // binary32: final result (one split) or this split's partial sums, straight from the accumulators.
-            float *out = p.splits > 1 ? p.partial + (int64_t)it.split * p.m * n : static_cast<float *>(p.out);
+            int split = it.split;
+            if constexpr (EXPERTS) split = it.split * p.experts + it.matrix;  // without partial sums the expert
+            float *out = p.splits > 1 ? p.partial + (int64_t)split * p.m * n
+                                      : static_cast<float *>(p.out) + (EXPERTS ? (int64_t)split * p.m * n : 0);
             const __amdgpu_buffer_rsrc_t rsrc_out = __builtin_amdgcn_make_buffer_rsrc(out + (int64_t)m_base * n + n_base, 0,
                                                                                       rows_in * n * 4, 0x00020000);
             const unsigned o_voff = (unsigned)(e_r * n + 4 * e_g) * 4;

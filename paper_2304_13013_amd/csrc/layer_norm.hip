@@ -1,0 +1,550 @@
+// Layer norm over the rows of a matrix, forward and backward, for gfx950.
+//
+//   mu = mean_j x,  r = 1 / sqrt(mean_j (x - mu)^2 + eps),  h = (x - mu) r,  y = h gamma + beta
+//   a = dy gamma,   dx = r (a - mean_j a - h mean_j(a h)),  dgamma_j = sum_i dy h,  dbeta_j = sum_i dy
+//
+// What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences
+// from it (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large).  Rows of up to 2048 columns
+// belong to a wave, up to 8192 to four and up to 16384 to eight; a group walks many rows, holds gamma and beta (or its
+// shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read from
+// L2 again.  Arithmetic is binary32; y and dx are rounded once.
+//
+// The sums over the rows: every workgroup adds its rows' terms in registers, its waves' sums meet in LDS and go to the
+// workspace, and a second launch adds those in a fixed order.  No atomics: the same inputs give the same bits.
+#include "sb_common.h"
+#include <type_traits>
+
+namespace sb {
+namespace {
+
+typedef unsigned short u16;
+
+template <class T>
+__device__ __forceinline__ float widen(T v) {
+    if constexpr (sizeof(T) == 2) return bf16_bits_to_float(v);
+    else return v;
+}
+// Element type T is u16 (bf16 bits) or float; a piece is V consecutive elements: 16 bytes, or one element where rows are not
+// multiples of that.
+template <class T, int V>
+struct Piece {
+    T e[V];
+};
+// ONCE: nobody reads it again.
+template <class T, int V, bool ONCE = true>
+__device__ __forceinline__ Piece<T, V> load_piece(const T *at) {
+    if constexpr (V == 1) {
+        return Piece<T, 1>{{ONCE ? __builtin_nontemporal_load(at) : *at}};
+    } else {
+        static_assert(sizeof(T) * V == 16, "16 bytes");
+        const v4u *from = reinterpret_cast<const v4u *>(at);
+        return __builtin_bit_cast(Piece<T, V>, ONCE ? __builtin_nontemporal_load(from) : *from);
+    }
+}
+template <class T, int V>
+__device__ __forceinline__ void store_piece(T *at, const float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (V == 4) *reinterpret_cast<v4f *>(at) = v4f{v[0], v[1], v[2], v[3]};
+        else *at = v[0];
+    } else {
+        if constexpr (V == 8) {
+            const v2u lo = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[0], v[1], v[2], v[3]}, v4bf));
+            const v2u hi = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[4], v[5], v[6], v[7]}, v4bf));
+            *reinterpret_cast<v4u *>(at) = v4u{lo.x, lo.y, hi.x, hi.y};
+        } else {
+            *at = __builtin_bit_cast(u16, (__bf16)v[0]);
+        }
+    }
+}
+// V elements of a binary32 vector; `at` is as aligned as the piece of the row that it goes with.
+template <int V>
+__device__ __forceinline__ void load_vector(const float *v, int at, float (&out)[V]) {
+    if constexpr (V == 1) {
+        out[0] = v[at];
+    } else {
+#pragma unroll
+        for (int q = 0; q < V; q += 4) {
+            const v4f x = *reinterpret_cast<const v4f *>(v + at + q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[q + e] = x[e];
+        }
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+// Sums of a group of WAVES waves, in every lane of it.  With more than one wave the group is the workgroup; `turn` alternates,
+// so that one barrier does: who writes a buffer again has passed the barrier of the call between.
+template <int WAVES, int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], float (*shared)[2][16], int turn) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) shared[turn][i][threadIdx.x >> 6] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = shared[turn][i][0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v[i] += shared[turn][i][w];
+        }
+    }
+}
+
+template <int WAVES>
+struct Group {
+    static constexpr int LANES = 64 * WAVES, THREADS = WAVES == 1 ? 256 : LANES, PER_BLOCK = THREADS / LANES;
+};
+
+// Rows of up to 64 * WAVES * V * P columns; P pieces a lane.  mean and rstd may be null, and gamma and beta.
+template <class T, int V, int P, int WAVES>
+__global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
+                                                                            const float *__restrict__ beta, float eps,
+                                                                            int64_t rows, int cols, T *__restrict__ y,
+                                                                            float *__restrict__ mean, float *__restrict__ rstd) {
+    typedef Group<WAVES> G;
+    __shared__ float shared[2][2][16];
+    const int lane = threadIdx.x % G::LANES;
+    const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)gridDim.x * G::PER_BLOCK;
+    float g[P][V], b[P][V];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = (lane + p * G::LANES) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[p][e] = 1.0f, b[p][e] = 0.0f;
+        if (c < cols) {
+            if (gamma != nullptr) load_vector<V>(gamma, c, g[p]);
+            if (beta != nullptr) load_vector<V>(beta, c, b[p]);
+        }
+    }
+    Piece<T, V> raw[P];
+    auto request = [&](int64_t row) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (lane + p * G::LANES) * V;
+            raw[p] = Piece<T, V>{};
+            if (c < cols) raw[p] = load_piece<T, V>(x + row * cols + c);
+        }
+    };
+    const float inv = 1.0f / (float)cols;
+    if (first < rows) request(first);
+    // All waves of a workgroup make the same number of rounds where they meet at barriers: WAVES > 1 has one row a workgroup.
+    for (int64_t row = first; row < rows; row += step) {
+        float v[P][V], s[1] = {0.0f};
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                v[p][e] = widen(raw[p].e[e]);
+                s[0] += v[p][e];
+            }
+        if (row + step < rows) request(row + step);
+        group_sums<WAVES, 1>(s, shared, 0);
+        const float mu = s[0] * inv;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool in = (lane + p * G::LANES) * V < cols;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                v[p][e] = in ? v[p][e] - mu : 0.0f;
+                s[0] = fmaf(v[p][e], v[p][e], s[0]);
+            }
+        }
+        group_sums<WAVES, 1>(s, shared, 1);
+        const float r = 1.0f / sqrtf(s[0] * inv + eps);
+        if (lane == 0) {
+            if (mean != nullptr) mean[row] = mu;
+            if (rstd != nullptr) rstd[row] = r;
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (lane + p * G::LANES) * V;
+            float out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = fmaf(v[p][e] * r, g[p][e], b[p][e]);
+            if (c < cols) store_piece<T, V>(y + row * cols + c, out);
+        }
+    }
+}
+
+// Rows that do not fit: three passes, of which two find the row in L2.
+template <class T, int V>
+__global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
+                                                               const float *__restrict__ beta, float eps, int64_t rows, int cols,
+                                                               T *__restrict__ y, float *__restrict__ mean,
+                                                               float *__restrict__ rstd) {
+    __shared__ float shared[2][2][16];
+    const float inv = 1.0f / (float)cols;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T *xr = x + row * cols;
+        float s[1] = {0.0f};
+        for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
+            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[0] += widen(q.e[e]);
+        }
+        group_sums<16, 1>(s, shared, 0);
+        const float mu = s[0] * inv;
+        s[0] = 0.0f;
+        for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
+            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = widen(q.e[e]) - mu;
+                s[0] = fmaf(d, d, s[0]);
+            }
+        }
+        group_sums<16, 1>(s, shared, 1);
+        const float r = 1.0f / sqrtf(s[0] * inv + eps);
+        if (threadIdx.x == 0) {
+            if (mean != nullptr) mean[row] = mu;
+            if (rstd != nullptr) rstd[row] = r;
+        }
+        for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
+            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+            float g[V], b[V], out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = 1.0f, b[e] = 0.0f;
+            if (gamma != nullptr) load_vector<V>(gamma, c, g);
+            if (beta != nullptr) load_vector<V>(beta, c, b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = fmaf((widen(q.e[e]) - mu) * r, g[e], b[e]);
+            store_piece<T, V>(y + row * cols + c, out);
+        }
+    }
+}
+
+// SUMS: the rows' terms of dgamma and dbeta are added up and left in partial[blockIdx.x][2][cols].  gamma lies in LDS, four
+// consecutive elements of a lane at a time and lanes side by side: in registers, next to the sums and two rows, it would
+// leave one wave per SIMD.
+template <class T, int V, int P, int WAVES, bool SUMS>
+__global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_backward_kernel(
+    const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean, const float *__restrict__ rstd,
+    const float *__restrict__ gamma, int64_t rows, int cols, T *__restrict__ dx, float *__restrict__ partial) {
+    typedef Group<WAVES> G;
+    constexpr int Q = V < 4 ? V : 4;
+    typedef float Quad __attribute__((ext_vector_type(Q)));
+    __shared__ float shared[2][2][16];
+    __shared__ Quad weights[P][V / Q][G::LANES];
+    const int lane = threadIdx.x % G::LANES;
+    const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)gridDim.x * G::PER_BLOCK;
+    float dg[SUMS ? P : 1][V], db[SUMS ? P : 1][V];
+    if (threadIdx.x < G::LANES) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int q = 0; q < V / Q; ++q) {
+                const int c = (lane + p * G::LANES) * V + q * Q;
+                Quad g;
+#pragma unroll
+                for (int e = 0; e < Q; ++e) g[e] = 1.0f;
+                if (c < cols && gamma != nullptr) g = *reinterpret_cast<const Quad *>(gamma + c);
+                weights[p][q][lane] = g;
+            }
+    }
+    if (SUMS)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < V; ++e) dg[p][e] = db[p][e] = 0.0f;
+    Piece<T, V> rx[P], rdy[P];
+    float mu = 0.0f, r = 0.0f;
+    auto request = [&](int64_t row) {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (lane + p * G::LANES) * V;
+            rx[p] = rdy[p] = Piece<T, V>{};
+            if (c < cols) {
+                rx[p] = load_piece<T, V>(x + row * cols + c);
+                rdy[p] = load_piece<T, V>(dy + row * cols + c);
+            }
+        }
+        mu = mean[row];
+        r = rstd[row];
+    };
+    const float inv = 1.0f / (float)cols;
+    if (first < rows) request(first);
+    __syncthreads();
+    int turn = 0;
+    for (int64_t row = first; row < rows; row += step, turn ^= 1) {
+        float h[P][V], d[P][V], s[2] = {0.0f, 0.0f};
+        const float r0 = r;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool in = (lane + p * G::LANES) * V < cols;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                d[p][e] = widen(rdy[p].e[e]);  // zero past the last column
+                h[p][e] = in ? (widen(rx[p].e[e]) - mu) * r : 0.0f;
+                const float a = d[p][e] * weights[p][e / Q][lane][e % Q];
+                s[0] += a;
+                s[1] = fmaf(a, h[p][e], s[1]);
+                if (SUMS) {
+                    dg[p][e] = fmaf(d[p][e], h[p][e], dg[p][e]);
+                    db[p][e] += d[p][e];
+                }
+            }
+        }
+        if (row + step < rows) request(row + step);
+        group_sums<WAVES, 2>(s, shared, turn);
+        const float sa = s[0] * inv, sh = s[1] * inv;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int c = (lane + p * G::LANES) * V;
+            float out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = r0 * (fmaf(d[p][e], weights[p][e / Q][lane][e % Q], -sa) - h[p][e] * sh);
+            if (c < cols) store_piece<T, V>(dx + row * cols + c, out);
+        }
+    }
+    if constexpr (SUMS) {
+        float *mine = partial + (int64_t)blockIdx.x * 2 * cols;
+        if constexpr (G::PER_BLOCK == 1) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int c = (lane + p * G::LANES) * V + e;
+                    if (c < cols) mine[c] = dg[p][e], mine[cols + c] = db[p][e];
+                }
+        } else {
+            // The waves' sums of a piece at a time, in wave order.
+            constexpr int SLOTS = G::LANES * V;
+            __shared__ float meet[G::PER_BLOCK][2][SLOTS];
+            const int wave = threadIdx.x / G::LANES;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    meet[wave][0][e * G::LANES + lane] = dg[p][e];
+                    meet[wave][1][e * G::LANES + lane] = db[p][e];
+                }
+                __syncthreads();
+                for (int i = threadIdx.x; i < 2 * SLOTS; i += G::THREADS) {
+                    const int which = i / SLOTS, slot = i % SLOTS;
+                    // Slot (column order): lane slot / V, element slot % V.
+                    const int at = (slot % V) * G::LANES + slot / V, c = p * SLOTS + slot;
+                    float sum = meet[0][which][at];
+#pragma unroll
+                    for (int w = 1; w < G::PER_BLOCK; ++w) sum += meet[w][which][at];
+                    if (c < cols) mine[which * cols + c] = sum;
+                }
+            }
+        }
+    }
+}
+
+// Rows that do not fit: two passes; the sums over the rows are another launch's.
+template <class T, int V>
+__global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T *__restrict__ dy, const T *__restrict__ x,
+                                                                        const float *__restrict__ mean,
+                                                                        const float *__restrict__ rstd,
+                                                                        const float *__restrict__ gamma, int64_t rows, int cols,
+                                                                        T *__restrict__ dx) {
+    __shared__ float shared[2][2][16];
+    const float inv = 1.0f / (float)cols;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+        const T *xr = x + row * cols, *dr = dy + row * cols;
+        const float mu = mean[row], r = rstd[row];
+        float s[2] = {0.0f, 0.0f};
+        for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
+            const Piece<T, V> q = load_piece<T, V, false>(xr + c), d = load_piece<T, V, false>(dr + c);
+            float g[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = 1.0f;
+            if (gamma != nullptr) load_vector<V>(gamma, c, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float a = widen(d.e[e]) * g[e];
+                s[0] += a;
+                s[1] = fmaf(a, (widen(q.e[e]) - mu) * r, s[1]);
+            }
+        }
+        group_sums<16, 2>(s, shared, turn);
+        const float sa = s[0] * inv, sh = s[1] * inv;
+        for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
+            const Piece<T, V> q = load_piece<T, V, false>(xr + c), d = load_piece<T, V, false>(dr + c);
+            float g[V], out[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) g[e] = 1.0f;
+            if (gamma != nullptr) load_vector<V>(gamma, c, g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) out[e] = r * (widen(d.e[e]) * g[e] - sa - (widen(q.e[e]) - mu) * r * sh);
+            store_piece<T, V>(dx + row * cols + c, out);
+        }
+    }
+}
+// partial[blockIdx.y][2][cols]: sums over the blockIdx.y-th share of the rows, a column a thread.
+template <class T>
+__global__ __launch_bounds__(256) void layer_norm_column_sums_kernel(const T *__restrict__ dy, const T *__restrict__ x,
+                                                                     const float *__restrict__ mean,
+                                                                     const float *__restrict__ rstd, int64_t rows, int cols,
+                                                                     float *__restrict__ partial) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float dg = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+        const float d = widen(dy[row * cols + c]);
+        dg = fmaf(d, (widen(x[row * cols + c]) - mean[row]) * rstd[row], dg);
+        db += d;
+    }
+    float *mine = partial + (int64_t)blockIdx.y * 2 * cols;
+    mine[c] = dg;
+    mine[cols + c] = db;
+}
+
+// dgamma and dbeta from `parts` partial sums [parts][2][cols]: 32 columns a workgroup, 32 runs of partial sums each, added in
+// order.  Either may be null.
+__global__ __launch_bounds__(1024) void layer_norm_reduce_kernel(const float *__restrict__ partial, int parts, int cols,
+                                                                 float *__restrict__ dgamma, float *__restrict__ dbeta) {
+    __shared__ float runs[32][33];
+    const int i = threadIdx.x & 31, run = threadIdx.x >> 5, total = 2 * cols;
+    const int at = blockIdx.x * 32 + i;
+    const int first = parts * run / 32, end = parts * (run + 1) / 32;
+    float sum = 0.0f;
+    if (at < total)
+        for (int k = first; k < end; ++k) sum += partial[(int64_t)k * total + at];
+    runs[run][i] = sum;
+    __syncthreads();
+    if (run == 0 && at < total) {
+#pragma unroll
+        for (int k = 1; k < 32; ++k) sum += runs[k][i];
+        float *out = at < cols ? dgamma : dbeta;
+        if (out != nullptr) out[at < cols ? at : at - cols] = sum;
+    }
+}
+
+constexpr int kLongParts = 256;  // shares of the rows where their sums are a launch of their own
+
+// Workgroups per compute unit that walk the rows: enough loads in flight, few partial sums.
+int walkers(int64_t rows, int per_block, int per_cu) {
+    const int64_t need = (rows + per_block - 1) / per_block, most = (int64_t)num_compute_units() * per_cu;
+    return (int)(need < most ? need : most);
+}
+
+// The group and the pieces for rows of `cols` columns, V elements a piece: calls f(integral constants P, WAVES), or returns
+// false for rows that do not fit.  A lane holds at most 32 elements; eight waves only of whole pieces (the others' 32 addresses
+// would not fit in its registers).
+template <int V, class F>
+bool with_group(int cols, F f) {
+    auto go = [&](auto elements, auto waves) {
+        constexpr int E = decltype(elements)::value, W = decltype(waves)::value;
+        if (cols > 64 * W * E) return false;
+        f(std::integral_constant<int, E / V>(), waves);
+        return true;
+    };
+    typedef std::integral_constant<int, 1> W1;
+    typedef std::integral_constant<int, 4> W4;
+    typedef std::integral_constant<int, 8> W8;
+    const bool done = go(std::integral_constant<int, 8>(), W1()) || go(std::integral_constant<int, 16>(), W1()) ||
+                      go(std::integral_constant<int, 24>(), W1()) || go(std::integral_constant<int, 32>(), W1()) ||
+                      go(std::integral_constant<int, 16>(), W4()) || go(std::integral_constant<int, 32>(), W4());
+    if constexpr (V > 1) return done || go(std::integral_constant<int, 32>(), W8());
+    return done;
+}
+// Columns of the longest rows that fit.
+int longest_row(bool whole) { return whole ? 16384 : 8192; }
+
+template <class T, int V>
+hipError_t forward_of(const T *x, const float *gamma, const float *beta, float eps, int64_t rows, int cols, T *y, float *mean,
+                      float *rstd, hipStream_t stream) {
+    const bool fits = with_group<V>(cols, [&](auto pieces, auto waves) {
+        constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
+        typedef Group<W> G;
+        layer_norm_kernel<T, V, P, W><<<walkers(rows, G::PER_BLOCK, W == 8 ? 4 : 8), G::THREADS, 0, stream>>>(
+            x, gamma, beta, eps, rows, cols, y, mean, rstd);
+    });
+    if (!fits)
+        layer_norm_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(x, gamma, beta, eps, rows, cols, y, mean, rstd);
+    return hipGetLastError();
+}
+
+// Workgroups of the backward pass, each of which leaves a pair of partial sums.
+int backward_blocks(int64_t rows, int cols, bool whole) {
+    if (cols > longest_row(whole)) return kLongParts;
+    return cols > 8192 ? walkers(rows, 1, 1) : cols > 2048 ? walkers(rows, 1, 2) : walkers(rows, 4, 2);
+}
+
+template <class T, int V>
+hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *rstd, const float *gamma, int64_t rows, int cols,
+                       T *dx, float *dgamma, float *dbeta, float *partial, hipStream_t stream) {
+    const bool sums = dgamma != nullptr || dbeta != nullptr;
+    const int blocks = backward_blocks(rows, cols, V > 1);
+    if (rows > 0) {
+        const bool fits = with_group<V>(cols, [&](auto pieces, auto waves) {
+            constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
+            typedef Group<W> G;
+            if (sums)
+                layer_norm_backward_kernel<T, V, P, W, true><<<blocks, G::THREADS, 0, stream>>>(dy, x, mean, rstd, gamma, rows,
+                                                                                                cols, dx, partial);
+            else
+                layer_norm_backward_kernel<T, V, P, W, false><<<blocks, G::THREADS, 0, stream>>>(dy, x, mean, rstd, gamma, rows,
+                                                                                                 cols, dx, nullptr);
+        });
+        if (!fits) {
+            layer_norm_backward_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);
+            if (sums)
+                layer_norm_column_sums_kernel<T><<<dim3((cols + 255) / 256, kLongParts), 256, 0, stream>>>(dy, x, mean, rstd, rows,
+                                                                                                          cols, partial);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (sums)
+        layer_norm_reduce_kernel<<<(2 * cols + 31) / 32, 1024, 0, stream>>>(partial, rows > 0 ? blocks : 0, cols, dgamma, dbeta);
+    return hipGetLastError();
+}
+
+bool whole_pieces(int64_t cols, bool bf16) { return cols % (bf16 ? 8 : 4) == 0; }
+
+}  // namespace
+
+size_t layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows <= 0) return 0;
+    // Either type: rows of whole pieces of four elements need not be of whole pieces of eight.
+    const int a = backward_blocks(rows, (int)cols, true), b = backward_blocks(rows, (int)cols, false);
+    return (size_t)(a > b ? a : b) * 2 * (size_t)cols * sizeof(float);
+}
+
+hipError_t launch_layer_norm(const void *x, const float *gamma, const float *beta, float eps, int64_t rows, int64_t cols, bool bf16,
+                             void *y, float *mean, float *rstd, hipStream_t stream) {
+    const bool whole = whole_pieces(cols, bf16);
+    if (bf16) {
+        const u16 *xs = static_cast<const u16 *>(x);
+        u16 *ys = static_cast<u16 *>(y);
+        return whole ? forward_of<u16, 8>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream)
+                     : forward_of<u16, 1>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream);
+    }
+    const float *xs = static_cast<const float *>(x);
+    float *ys = static_cast<float *>(y);
+    return whole ? forward_of<float, 4>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream)
+                 : forward_of<float, 1>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream);
+}
+
+hipError_t launch_layer_norm_backward(const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma,
+                                      int64_t rows, int64_t cols, bool bf16, void *dx, float *dgamma, float *dbeta, void *ws,
+                                      hipStream_t stream) {
+    const bool whole = whole_pieces(cols, bf16);
+    float *partial = static_cast<float *>(ws);
+    if (bf16) {
+        const u16 *d = static_cast<const u16 *>(dy), *xs = static_cast<const u16 *>(x);
+        u16 *out = static_cast<u16 *>(dx);
+        return whole ? backward_of<u16, 8>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream)
+                     : backward_of<u16, 1>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream);
+    }
+    const float *d = static_cast<const float *>(dy), *xs = static_cast<const float *>(x);
+    float *out = static_cast<float *>(dx);
+    return whole ? backward_of<float, 4>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream)
+                 : backward_of<float, 1>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream);
+}
+
+}  // namespace sb

@@ -77,6 +77,36 @@ size_t gemm_bf16_tn_workspace_bytes(const WeightGradPlan &plan, int64_t n, int64
 hipError_t launch_gemm_bf16_tn(const WeightGradPlan &plan, const void *dy, const void *x, int64_t b, int64_t n, int64_t m, void *dw,
                                sb_dtype dw_dtype, void *ws, hipStream_t stream);
 
+// The same with a gradient per expert: rows offsets[e] .. offsets[e + 1] - 1 (device) of dy and x give dw[e]; dw [experts,m,n].
+struct ExpertGradPlan {
+    bool small;  // 128x128 tiles, else 256x256
+    int splits;
+};
+ExpertGradPlan plan_gemm_bf16_tn_experts(int64_t b, int64_t n, int64_t m, int64_t experts);
+size_t gemm_bf16_tn_experts_workspace_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts);
+hipError_t launch_gemm_bf16_tn_experts(const ExpertGradPlan &plan, const void *dy, const void *x, const int32_t *offsets, int64_t experts,
+                                       int64_t b, int64_t n, int64_t m, void *dw, sb_dtype dw_dtype, void *ws, hipStream_t stream);
+
+// The float8 layer with a scale for each block of 128 (quantize_block.hip, gemm_f8_block.hip).  fmt 0: E4M3, 1: E5M2.
+hipError_t launch_quantize_rows_block(const void *x, int64_t rows, int64_t cols, int fmt, uint8_t *codes, uint8_t *scales,
+                                      hipStream_t stream);
+// X [rows,n] and W [experts,m,n] in one launch; rows may be 0, wq_t and scales_wt null.
+hipError_t launch_quantize_block(const void *x, int64_t rows, int fmt_x, uint8_t *xq, uint8_t *scales_x, const void *w, int64_t experts,
+                                 int64_t m, int64_t n, int fmt_w, uint8_t *wq, uint8_t *scales_w, uint8_t *wq_t, uint8_t *scales_wt,
+                                 hipStream_t stream);
+// offsets null: one b for all rows (experts == 1).
+hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *scales_a, const uint8_t *bq, int fmt_b,
+                                const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M, int64_t N, int64_t K,
+                                void *out, sb_dtype out_dtype, hipStream_t stream);
+
+// Layer norm (layer_norm.hip): x and y bf16 or f32; gamma, beta, mean, rstd may be null where the C ABI allows it.
+hipError_t launch_layer_norm(const void *x, const float *gamma, const float *beta, float eps, int64_t rows, int64_t cols, bool bf16,
+                             void *y, float *mean, float *rstd, hipStream_t stream);
+size_t layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_layer_norm_backward(const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma,
+                                      int64_t rows, int64_t cols, bool bf16, void *dx, float *dgamma, float *dbeta, void *ws,
+                                      hipStream_t stream);
+
 size_t stable_adamw_workspace_bytes();
 // b1_hat / b2_hat are the corrected decay rates, omb1 / omb2 their complements to one (all formed by the caller).
 hipError_t launch_stable_adamw_step(float *theta, float *v, float *u, const void *grad, bool grad_bf16, int64_t count,

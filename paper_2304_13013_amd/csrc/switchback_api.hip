@@ -54,6 +54,26 @@ int weight_gradient_workspace_status(const sb::WeightGradPlan &plan, int64_t n, 
     return ws_bytes < need ? SB_WORKSPACE_TOO_SMALL : SB_OK;
 }
 
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+int64_t whole_blocks(int64_t cols) { return (cols + 127) / 128 * 128; }
+
+// Shapes of the block-scaled layer: those of the others, and the weights' codes below 2^32 bytes per expert.
+int block_shape_status(int64_t b, int64_t n, int64_t m, int64_t experts, bool grouped) {
+    const int st = layer_shape_status(b, n, m);
+    if (st != SB_OK) return st;
+    if (experts < 1 || (!grouped && experts != 1)) return SB_INVALID_ARG;
+    if (experts > 1024 || (m + 256) * whole_blocks(n) >= (int64_t)1 << 32 || (n + 256) * whole_blocks(m) >= (int64_t)1 << 32 ||
+        experts * ((m + 63) / 64) * ((n + 63) / 64) > (int64_t)1 << 28)
+        return SB_UNSUPPORTED_SHAPE;
+    return SB_OK;
+}
+
+// Codes of [rows,cols] by rows, then their scales, in a workspace.
+size_t row_codes_bytes(int64_t rows, int64_t cols) { return ((size_t)rows * (size_t)whole_blocks(cols) + 255) / 256 * 256; }
+size_t block_workspace_bytes(int64_t rows, int64_t cols) {
+    return row_codes_bytes(rows, cols) + (size_t)rows * (size_t)((cols + 511) / 512 * 4);
+}
+
 int from_hip(hipError_t e) { return e == hipSuccess ? SB_OK : SB_HIP_ERROR; }
 
 // Corrected decay rate of StableAdamW, in binary64: beta (1 - beta^(t-1)) / (1 - beta^t); 0 at t = 1.
@@ -394,6 +414,128 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
                                                saved->state_w, b, n, m, dx, dx_dtype, s));
 }
 
+int switchback_quantize_rowwise_f8_block(const void *x_bf16, int64_t rows, int64_t cols, sb_f8_format fmt, uint8_t *codes,
+                                         uint8_t *scales, void *stream) {
+    if (rows < 0 || cols <= 0 || !ok_f8(fmt)) return SB_INVALID_ARG;
+    if (cols % 8 || cols > kMaxIntK || rows > (int64_t)1 << 30 || rows * ((cols + 511) / 512) > (int64_t)1 << 32)
+        return SB_UNSUPPORTED_SHAPE;
+    if (rows == 0) return SB_OK;
+    if (!ok_ptr(x_bf16) || !ok_ptr(codes) || !ok_ptr(scales)) return SB_INVALID_ARG;
+    return from_hip(sb::launch_quantize_rows_block(x_bf16, rows, cols, fmt, codes, scales, static_cast<hipStream_t>(stream)));
+}
+
+int switchback_quantize_weight_f8_block(const void *w_bf16, int64_t experts, int64_t m, int64_t n, sb_f8_format fmt,
+                                        uint8_t *codes, uint8_t *scales, uint8_t *codes_t, uint8_t *scales_t, void *stream) {
+    if (!ok_f8(fmt)) return SB_INVALID_ARG;
+    const int st = block_shape_status(0, n, m, experts, true);
+    if (st != SB_OK) return st;
+    if (!ok_ptr(w_bf16) || !ok_ptr(codes) || !ok_ptr(scales)) return SB_INVALID_ARG;
+    if ((codes_t == nullptr) != (scales_t == nullptr) || (codes_t != nullptr && (!ok_ptr(codes_t) || !ok_ptr(scales_t))))
+        return SB_INVALID_ARG;
+    return from_hip(sb::launch_quantize_block(nullptr, 0, SB_E4M3, nullptr, nullptr, w_bf16, experts, m, n, fmt, codes, scales,
+                                              codes_t, scales_t, static_cast<hipStream_t>(stream)));
+}
+
+int switchback_matmul_f8_block(const uint8_t *aq, sb_f8_format fmt_a, const uint8_t *scales_a, const uint8_t *bq,
+                               sb_f8_format fmt_b, const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M,
+                               int64_t N, int64_t K, void *out, sb_dtype out_dtype, void *stream) {
+    if (!ok_f8(fmt_a) || !ok_f8(fmt_b) || (out_dtype != SB_BF16 && out_dtype != SB_F32)) return SB_INVALID_ARG;
+    const int st = block_shape_status(M, K, N, experts, offsets != nullptr);
+    if (st != SB_OK) return st;
+    if (K % 128) return SB_UNSUPPORTED_SHAPE;
+    if (M == 0) return SB_OK;
+    if (!ok_ptr(aq) || !ok_ptr(scales_a) || !ok_ptr(bq) || !ok_ptr(scales_b) || !ok_ptr(out) || !aligned4(offsets))
+        return SB_INVALID_ARG;
+    return from_hip(sb::launch_gemm_f8_block(aq, fmt_a, scales_a, bq, fmt_b, scales_b, offsets, experts, M, N, K, out, out_dtype,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint8_t *scales_w, const int32_t *offsets,
+                               int64_t experts, int64_t b, int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, void *y,
+                               sb_dtype y_dtype, void *ws, size_t ws_bytes, void *stream) {
+    if (!ok_f8(fmt_x) || !ok_f8(fmt_w) || (y_dtype != SB_BF16 && y_dtype != SB_F32)) return SB_INVALID_ARG;
+    const int st = block_shape_status(b, n, m, experts, offsets != nullptr);
+    if (st != SB_OK) return st;
+    if (b == 0) return SB_OK;
+    if (!ok_ptr(x_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w) || !ok_ptr(y) || !ok_ptr(ws) || !aligned4(offsets)) return SB_INVALID_ARG;
+    if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *xq = static_cast<uint8_t *>(ws), *scales_x = xq + row_codes_bytes(b, n);
+    const hipError_t e = sb::launch_quantize_rows_block(x_bf16, b, n, fmt_x, xq, scales_x, s);
+    if (e != hipSuccess) return SB_HIP_ERROR;
+    return from_hip(sb::launch_gemm_f8_block(xq, fmt_x, scales_x, wq, fmt_w, scales_w, offsets, experts, b, m, whole_blocks(n), y,
+                                             y_dtype, s));
+}
+
+int switchback_forward_f8_block(const void *x_bf16, const void *w_bf16, const int32_t *offsets, int64_t experts, int64_t b,
+                                int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, uint8_t *wq, uint8_t *scales_w,
+                                uint8_t *wq_t, uint8_t *scales_wt, void *y, sb_dtype y_dtype, void *ws, size_t ws_bytes,
+                                void *stream) {
+    if (!ok_f8(fmt_x) || !ok_f8(fmt_w) || (y_dtype != SB_BF16 && y_dtype != SB_F32)) return SB_INVALID_ARG;
+    const int st = block_shape_status(b, n, m, experts, offsets != nullptr);
+    if (st != SB_OK) return st;
+    if (!ok_ptr(w_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w)) return SB_INVALID_ARG;
+    if ((wq_t == nullptr) != (scales_wt == nullptr) || (wq_t != nullptr && (!ok_ptr(wq_t) || !ok_ptr(scales_wt))))
+        return SB_INVALID_ARG;
+    if (b > 0 && (!ok_ptr(x_bf16) || !ok_ptr(y) || !ok_ptr(ws) || !aligned4(offsets))) return SB_INVALID_ARG;
+    if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *xq = static_cast<uint8_t *>(ws), *scales_x = b > 0 ? xq + row_codes_bytes(b, n) : nullptr;
+    const hipError_t e = sb::launch_quantize_block(x_bf16, b, fmt_x, xq, scales_x, w_bf16, experts, m, n, fmt_w, wq, scales_w, wq_t,
+                                                   scales_wt, s);
+    if (e != hipSuccess) return SB_HIP_ERROR;
+    if (b == 0) return SB_OK;
+    return from_hip(sb::launch_gemm_f8_block(xq, fmt_x, scales_x, wq, fmt_w, scales_w, offsets, experts, b, m, whole_blocks(n), y,
+                                             y_dtype, s));
+}
+
+int switchback_backward_weight_experts(const void *dy_bf16, const void *x_bf16, const int32_t *offsets, int64_t experts,
+                                       int64_t b, int64_t n, int64_t m, void *dw, sb_dtype dw_dtype, void *ws, size_t ws_bytes,
+                                       void *stream) {
+    if (dw_dtype != SB_BF16 && dw_dtype != SB_F32) return SB_INVALID_ARG;
+    const int st = block_shape_status(b, n, m, experts, true);
+    if (st != SB_OK) return st;
+    if (!ok_ptr(dw) || offsets == nullptr || !aligned4(offsets) || (b > 0 && (!ok_ptr(dy_bf16) || !ok_ptr(x_bf16))))
+        return SB_INVALID_ARG;
+    const sb::ExpertGradPlan plan = sb::plan_gemm_bf16_tn_experts(b, n, m, experts);
+    const size_t need = sb::gemm_bf16_tn_experts_workspace_bytes(plan, n, m, experts);
+    if (need > 0 && (ws == nullptr || !aligned16(ws))) return SB_INVALID_ARG;
+    if (ws_bytes < need) return SB_WORKSPACE_TOO_SMALL;
+    return from_hip(sb::launch_gemm_bf16_tn_experts(plan, dy_bf16, x_bf16, offsets, experts, b, n, m, dw, dw_dtype, ws,
+                                                    static_cast<hipStream_t>(stream)));
+}
+
+size_t switchback_backward_weight_experts_workspace_bytes(int64_t b, int64_t n, int64_t m, int64_t experts) {
+    if (block_shape_status(b, n, m, experts, true) != SB_OK) return 0;
+    return sb::gemm_bf16_tn_experts_workspace_bytes(sb::plan_gemm_bf16_tn_experts(b, n, m, experts), n, m, experts);
+}
+
+int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, const float *beta, float eps, int64_t rows,
+                          int64_t cols, void *y, float *mean, float *rstd, void *stream) {
+    if (rows < 0 || cols <= 0 || (dtype != SB_BF16 && dtype != SB_F32) || !(eps > 0.0f) || !std::isfinite(eps)) return SB_INVALID_ARG;
+    if (cols > 65536 || rows > (int64_t)1 << 30) return SB_UNSUPPORTED_SHAPE;
+    if (rows == 0) return SB_OK;
+    if (!ok_ptr(x) || !ok_ptr(y) || !aligned16(gamma) || !aligned16(beta) || !aligned4(mean) || !aligned4(rstd)) return SB_INVALID_ARG;
+    return from_hip(sb::launch_layer_norm(x, gamma, beta, eps, rows, cols, dtype == SB_BF16, y, mean, rstd,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype, const float *mean, const float *rstd,
+                                   const float *gamma, int64_t rows, int64_t cols, void *dx, float *dgamma, float *dbeta,
+                                   void *ws, size_t ws_bytes, void *stream) {
+    if (rows < 0 || cols <= 0 || (dtype != SB_BF16 && dtype != SB_F32)) return SB_INVALID_ARG;
+    if (cols > 65536 || rows > (int64_t)1 << 30) return SB_UNSUPPORTED_SHAPE;
+    const bool sums = dgamma != nullptr || dbeta != nullptr;
+    if (rows > 0 && (!ok_ptr(dy) || !ok_ptr(x) || !ok_ptr(dx) || mean == nullptr || rstd == nullptr)) return SB_INVALID_ARG;
+    if (!aligned16(gamma) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dgamma) || !aligned4(dbeta)) return SB_INVALID_ARG;
+    if (sums && rows > 0) {
+        if (!ok_ptr(ws)) return SB_INVALID_ARG;
+        if (ws_bytes < sb::layer_norm_backward_workspace_bytes(rows, cols)) return SB_WORKSPACE_TOO_SMALL;
+    }
+    return from_hip(sb::launch_layer_norm_backward(dy, x, mean, rstd, gamma, rows, cols, dtype == SB_BF16, dx, dgamma, dbeta, ws,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
 int switchback_stable_adamw_step(float *theta, float *v, float *u, const void *grad, sb_dtype grad_dtype,
                                  int64_t count, float alpha, float beta1, float beta2, float eps, float lambda,
                                  int64_t t, float *rms_out, void *ws, size_t ws_bytes, void *stream) {
@@ -454,6 +596,12 @@ size_t switchback_workspace_bytes(int op, int64_t b, int64_t n, int64_t m) {
             if (n <= 0 || m <= 0) return 0;
             return sb::quantize_colwise_workspace_bytes(m, n);
         case SB_OP_STABLE_ADAMW: return sb::stable_adamw_workspace_bytes();
+        case SB_OP_LAYER_NORM_BACKWARD:  // x is [b, n]
+            if (b < 0 || n <= 0 || n > 65536) return 0;
+            return sb::layer_norm_backward_workspace_bytes(b, n);
+        case SB_OP_LINEAR_F8_BLOCK:
+            if (b < 0 || n <= 0) return 0;
+            return block_workspace_bytes(b, n);
         default: return 0;
     }
 }

@@ -4,7 +4,8 @@ torch is used for device memory and the current HIP stream; every step of the la
 kernels.  There is no CPU or eager fallback: if the built library or the GPU is missing, the calls raise.
 
 Names follow the C ABI: quantize_rowwise, quantize_tensorwise, matmul_int8_dequant, forward, backward_input,
-backward_weight (Algorithm 1 of arxiv 2304.13013: X [b,n], W [m,n], Y/dY [b,m]).
+backward_weight (Algorithm 1 of arxiv 2304.13013: X [b,n], W [m,n], Y/dY [b,m]); its variants; the float8 layer with a scale
+for each block of 128, also with a weight per expert; layer norm with its gradients.
 """
 import ctypes
 import importlib.util
@@ -20,6 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libswitchback.so")
 SB_BF16, SB_F32, SB_I32_RAW = 0, 1, 2
 SB_OP_QUANTIZE_TENSORWISE, SB_OP_FORWARD, SB_OP_BACKWARD_INPUT, SB_OP_BACKWARD_WEIGHT, SB_OP_QUANTIZE_COLWISE = 0, 1, 2, 3, 4
 SB_OP_STABLE_ADAMW = 5
+SB_OP_LAYER_NORM_BACKWARD, SB_OP_LINEAR_F8_BLOCK = 6, 7
 SB_E4M3, SB_E5M2 = 0, 1
 
 _TORCH_DTYPE = {SB_BF16: torch.bfloat16, SB_F32: torch.float32, SB_I32_RAW: torch.int32}
@@ -80,6 +82,16 @@ def load_library():
     lib.switchback_stable_adamw_plan.restype = i64
     lib.switchback_stable_adamw_step_multi.argtypes = [vp, ci, i64, ci, cf, cf, cf, cf, cf, i64, vp, vp, sz, vp]
     lib.switchback_stable_adamw_step_multi.restype = ci
+    lib.switchback_quantize_rowwise_f8_block.argtypes = [vp, i64, i64, ci, vp, vp, vp]
+    lib.switchback_quantize_weight_f8_block.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp, vp, vp]
+    lib.switchback_matmul_f8_block.argtypes = [vp, ci, vp, vp, ci, vp, vp, i64, i64, i64, i64, vp, ci, vp]
+    lib.switchback_linear_f8_block.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, ci, vp, sz, vp]
+    lib.switchback_forward_f8_block.argtypes = [vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, ci, vp, sz, vp]
+    lib.switchback_backward_weight_experts.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, ci, vp, sz, vp]
+    lib.switchback_backward_weight_experts_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.switchback_backward_weight_experts_workspace_bytes.restype = sz
+    lib.switchback_layer_norm.argtypes = [vp, ci, vp, vp, cf, i64, i64, vp, vp, vp, vp]
+    lib.switchback_layer_norm_backward.argtypes = [vp, vp, ci, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.switchback_ceiling_mfma.argtypes = [ci, vp, sz, vp, sz, ci, ci, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.switchback_ceiling_mfma.restype = ci
     lib.switchback_ceiling_copy.argtypes = [vp, vp, sz, vp]
@@ -95,7 +107,10 @@ def load_library():
                  "switchback_quantize_colwise_transpose", "switchback_matmul_int8_dequant_rc",
                  "switchback_forward_q", "switchback_backward_input_q", "switchback_stable_adamw_step",
                  "switchback_quantize_rowwise_f8", "switchback_quantize_tensorwise_f8", "switchback_matmul_f8_dequant",
-                 "switchback_forward_f8", "switchback_backward_input_f8"):
+                 "switchback_forward_f8", "switchback_backward_input_f8", "switchback_quantize_rowwise_f8_block",
+                 "switchback_quantize_weight_f8_block", "switchback_matmul_f8_block", "switchback_linear_f8_block",
+                 "switchback_forward_f8_block", "switchback_backward_weight_experts", "switchback_layer_norm",
+                 "switchback_layer_norm_backward"):
         getattr(lib, name).restype = ci
     _lib = lib
     return lib
@@ -159,6 +174,7 @@ def _stream_getter(torch_c):
 
 
 _stream = _stream_getter(torch._C)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _dev_general(t, dtype, ndim=None):
@@ -562,6 +578,265 @@ def backward_input_f8(dy, bufs, dx=None, dx_dtype=torch.bfloat16, fmt_g=SB_E5M2,
                                             _dev(dx, dx_dtype, 2), _SB_DTYPE[dx_dtype], _ptr(bufs.gq),
                                             _ptr(bufs.state_g), fmt_g, fmt_w, _stream()))
     return dx
+
+
+# ---- float8 with a scale for each block of 128, plain or with a weight per expert -----------------------------------
+# Codes are uint8 tensors with rows of whole blocks (zeros behind the row's end), scales uint8 exponents e + 127: a block
+# stands for value(code) * 2^e.  Weights of experts are [experts, m, n] and go with `offsets`, int32 [experts + 1] on the GPU:
+# rows offsets[e] .. offsets[e + 1] - 1 are expert e's, rows past the last offset no one's, whose outputs stay as they were.
+
+def _on_current_device(*tensors):
+    """The calls below enqueue on the current device's stream: their tensors have to be there (those on no GPU at all, -1, are
+    refused by the other checks)."""
+    at = {t.get_device() for t in tensors if t is not None} - {-1}
+    if at and at != {_current_device()}:
+        raise SwitchBackError("tensors live on GPU %s, the current device is %d" % (sorted(at), _current_device()))
+
+
+def _whole_blocks(cols):
+    return -(-cols // 128) * 128
+
+
+def _scale_pitch(cols):
+    return -(-cols // 512) * 4
+
+
+def _offsets(offsets, lead):
+    """Pointer to the offsets of weights (or codes) with leading dimensions `lead`: none, or the number of experts."""
+    if not lead:
+        if offsets is not None:
+            raise SwitchBackError("offsets go with a weight per expert, [experts, ., .]")
+        return None
+    if offsets is None:
+        raise SwitchBackError("weights of experts need offsets")
+    if offsets.numel() != lead[0] + 1:
+        raise SwitchBackError("offsets must hold %d entries, got %d" % (lead[0] + 1, offsets.numel()))
+    return _dev(offsets, torch.int32, 1)
+
+
+def _weight_shape(w):
+    """Leading dimensions, experts and both widths of a weight (or its codes)."""
+    if w.dim() not in (2, 3):
+        raise SwitchBackError("expected a weight [m, n] or [experts, m, n], got %s" % (tuple(w.shape),))
+    lead = tuple(w.shape[:-2])
+    return lead, (lead[0] if lead else 1), w.shape[-2], w.shape[-1]
+
+
+def quantize_rowwise_f8_block(x, fmt, codes=None, scales=None):
+    """Blocks of 1 x 128 of a bf16 [rows, cols] tensor -> (codes [rows, K], scales [rows, S]); K is cols rounded up to a
+    multiple of 128, S = K / 128 rounded up to a multiple of 4."""
+    lib = _entries()
+    rows, cols = x.shape
+    codes = _out(codes, (rows, _whole_blocks(cols)), torch.uint8, x.device, "codes")
+    scales = _out(scales, (rows, _scale_pitch(cols)), torch.uint8, x.device, "scales")
+    _on_current_device(x, codes, scales)
+    _check(lib.switchback_quantize_rowwise_f8_block(_dev(x, torch.bfloat16, 2), rows, cols, fmt, _dev(codes, torch.uint8),
+                                                    _dev(scales, torch.uint8), _stream()))
+    return codes, scales
+
+
+def quantize_weight_f8_block(w, fmt, codes=None, scales=None, codes_t=None, scales_t=None, transpose=True):
+    """Blocks of 128 x 128 of a bf16 weight [m, n] or [experts, m, n] -> (codes [.., m, K], scales [.., blocks of m, K / 128],
+    and the same of the transpose, [.., n, K'] and [.., blocks of n, K' / 128], or None, None)."""
+    lib = _entries()
+    lead, experts, m, n = _weight_shape(w)
+    km, kn = _whole_blocks(m), _whole_blocks(n)
+    codes = _out(codes, lead + (m, kn), torch.uint8, w.device, "codes")
+    scales = _out(scales, lead + (km // 128, kn // 128), torch.uint8, w.device, "scales")
+    if transpose or codes_t is not None or scales_t is not None:
+        codes_t = _out(codes_t, lead + (n, km), torch.uint8, w.device, "codes_t")
+        scales_t = _out(scales_t, lead + (kn // 128, km // 128), torch.uint8, w.device, "scales_t")
+    _on_current_device(w, codes, scales, codes_t, scales_t)
+    _check(lib.switchback_quantize_weight_f8_block(
+        _dev(w, torch.bfloat16), experts, m, n, fmt, _dev(codes, torch.uint8), _dev(scales, torch.uint8),
+        _dev(codes_t, torch.uint8) if codes_t is not None else None,
+        _dev(scales_t, torch.uint8) if scales_t is not None else None, _stream()))
+    return codes, scales, codes_t, scales_t
+
+
+def _check_weight_scales(scales, lead, m, k, device):
+    _out(scales, lead + (_whole_blocks(m) // 128, k // 128), torch.uint8, device, "scales of the weight")
+    return _dev(scales, torch.uint8)
+
+
+def matmul_f8_block(aq, fmt_a, scales_a, bq, fmt_b, scales_b, offsets=None, out=None, out_dtype=torch.bfloat16):
+    """out[i,j] = sum over blocks of 2^(ea + eb) sum_k aq[i,k] bq[j,k], with rows by expert if bq is [experts, N, K]."""
+    lib = _entries()
+    M, K = aq.shape
+    lead, experts, N, kb = _weight_shape(bq)
+    if kb != K:
+        raise SwitchBackError("aq [M,K] and bq [..,N,K] disagree on K")
+    where = _offsets(offsets, lead)
+    out_dtype = out_dtype if out is None else out.dtype
+    if out_dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("out must be bf16 or f32")
+    out = _out(out, (M, N), out_dtype, aq.device, "out")
+    _out(scales_a, (M, _scale_pitch(K)), torch.uint8, aq.device, "scales_a")
+    _on_current_device(aq, scales_a, bq, scales_b, offsets, out)
+    _check(lib.switchback_matmul_f8_block(
+        _dev(aq, torch.uint8, 2), fmt_a, _dev(scales_a, torch.uint8), _dev(bq, torch.uint8), fmt_b,
+        _check_weight_scales(scales_b, lead, N, K, aq.device), where, experts, M, N, K, _dev(out, out_dtype, 2),
+        _SB_DTYPE[out_dtype], _stream()))
+    return out
+
+
+def linear_f8_block(x, wq, scales_w, offsets=None, fmt_x=SB_E4M3, fmt_w=SB_E4M3, y=None, y_dtype=torch.bfloat16, ws=None):
+    """Y = X W^T with codes of W that are kept (quantize_weight_f8_block), X [b,n] bf16 quantized on the way: serving."""
+    lib = _entries()
+    b, n = x.shape
+    lead, experts, m, k = _weight_shape(wq)
+    if k != _whole_blocks(n):
+        raise SwitchBackError("x has %d columns, the codes are for %d" % (n, k))
+    where = _offsets(offsets, lead)
+    y_dtype = y_dtype if y is None else y.dtype
+    if y_dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("y must be bf16 or f32")
+    y = _out(y, (b, m), y_dtype, x.device, "y")
+    ws = _workspace(SB_OP_LINEAR_F8_BLOCK, b, n, 0, x.device) if ws is None else ws
+    _on_current_device(x, wq, scales_w, offsets, y, ws)
+    _check(lib.switchback_linear_f8_block(
+        _dev(x, torch.bfloat16, 2), _dev(wq, torch.uint8), _check_weight_scales(scales_w, lead, m, k, x.device), where, experts,
+        b, n, m, fmt_x, fmt_w, _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+    return y
+
+
+class BlockBuffers:
+    """Device buffers of one block-scaled float8 layer of shape (b, n, m), or of `experts` such layers that share b rows,
+    allocated once: the weight's codes and scales in both layouts, and the workspaces."""
+
+    def __init__(self, b, n, m, experts=None, device="cuda"):
+        self.b, self.n, self.m, self.experts = b, n, m, experts
+        lead, km, kn = (() if experts is None else (experts,)), _whole_blocks(m), _whole_blocks(n)
+        e = lambda *shape: torch.empty(lead + shape, dtype=torch.uint8, device=device)
+        self.wq, self.scales_w = e(m, kn), e(km // 128, kn // 128)
+        self.wq_t, self.scales_wt = e(n, km), e(kn // 128, km // 128)
+        self.ws = torch.empty(max(workspace_bytes(SB_OP_LINEAR_F8_BLOCK, b, n, 0), workspace_bytes(SB_OP_LINEAR_F8_BLOCK, b, m, 0), 16),
+                              dtype=torch.uint8, device=device)
+        self.ws_dw = (_workspace(SB_OP_BACKWARD_WEIGHT, b, n, m, device) if experts is None else
+                      _experts_workspace(b, n, m, experts, device))
+
+
+def _check_block_bufs(bufs, b, n, m, lead):
+    _check_bufs(bufs, b, n, m)
+    if bufs.experts != (lead[0] if lead else None):
+        raise SwitchBackError("layer buffers are for %s experts, the weight is %s" % (bufs.experts, lead or "plain"))
+
+
+def forward_f8_block(x, w, bufs=None, offsets=None, y=None, y_dtype=torch.bfloat16, fmt_x=SB_E4M3, fmt_w=SB_E4M3):
+    """Forward pass with a scale for each block of 128; w [m,n], or [experts,m,n] with offsets.  Returns (y [b,m], bufs); bufs
+    (BlockBuffers) holds the codes of W and of its transpose."""
+    lib = _entries()
+    b, n = x.shape
+    lead, experts, m, k = _weight_shape(w)
+    if k != n:
+        raise SwitchBackError("x [b,n] and w [..,m,n] disagree on n")
+    where = _offsets(offsets, lead)
+    bufs = BlockBuffers(b, n, m, lead[0] if lead else None, x.device) if bufs is None else bufs
+    _check_block_bufs(bufs, b, n, m, lead)
+    y_dtype = y_dtype if y is None else y.dtype
+    if y_dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("y must be bf16 or f32")
+    y = _out(y, (b, m), y_dtype, x.device, "y")
+    _on_current_device(x, w, offsets, y, bufs.wq)
+    _check(lib.switchback_forward_f8_block(
+        _dev(x, torch.bfloat16, 2), _dev(w, torch.bfloat16), where, experts, b, n, m, fmt_x, fmt_w, _ptr(bufs.wq),
+        _ptr(bufs.scales_w), _ptr(bufs.wq_t), _ptr(bufs.scales_wt), _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(bufs.ws),
+        bufs.ws.numel(), _stream()))
+    return y, bufs
+
+
+def backward_input_f8_block(dy, bufs, offsets=None, dx=None, dx_dtype=torch.bfloat16, fmt_g=SB_E5M2, fmt_w=SB_E4M3):
+    """Input gradient with the codes that forward_f8_block left in bufs (fmt_w as there).  Returns dx [b,n]."""
+    lib = _entries()
+    b, m = dy.shape
+    _check_bufs(bufs, b, bufs.n, m)
+    lead = () if bufs.experts is None else (bufs.experts,)
+    where = _offsets(offsets, lead)
+    dx_dtype = dx_dtype if dx is None else dx.dtype
+    if dx_dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("dx must be bf16 or f32")
+    dx = _out(dx, (b, bufs.n), dx_dtype, dy.device, "dx")
+    _on_current_device(dy, offsets, dx, bufs.wq)
+    _check(lib.switchback_linear_f8_block(
+        _dev(dy, torch.bfloat16, 2), _ptr(bufs.wq_t), _ptr(bufs.scales_wt), where, bufs.experts or 1, b, m, bufs.n, fmt_g, fmt_w,
+        _dev(dx, dx_dtype, 2), _SB_DTYPE[dx_dtype], _ptr(bufs.ws), bufs.ws.numel(), _stream()))
+    return dx
+
+
+def _experts_workspace(b, n, m, experts, device):
+    need = int(load_library().switchback_backward_weight_experts_workspace_bytes(b, n, m, experts))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+
+
+def backward_weight_experts(dy, x, offsets, bufs=None, dw=None, dw_dtype=torch.bfloat16):
+    """The 16-bit weight gradient per expert: dw[e] = dY^T X over rows offsets[e] .. offsets[e+1] - 1 -> [experts, m, n]."""
+    lib = _entries()
+    b, m = dy.shape
+    n = x.shape[1]
+    if x.shape[0] != b:
+        raise SwitchBackError("dy [b,m] and x [b,n] disagree on b")
+    where = _dev(offsets, torch.int32, 1)
+    experts = offsets.numel() - 1
+    if bufs is not None:
+        _check_block_bufs(bufs, b, n, m, (experts,))
+    ws = bufs.ws_dw if bufs is not None else _experts_workspace(b, n, m, experts, dy.device)
+    dw_dtype = dw_dtype if dw is None else dw.dtype
+    if dw_dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("dw must be bf16 or f32")
+    dw = _out(dw, (experts, m, n), dw_dtype, dy.device, "dw")
+    _on_current_device(dy, x, offsets, dw, ws)
+    _check(lib.switchback_backward_weight_experts(_dev(dy, torch.bfloat16, 2), _dev(x, torch.bfloat16, 2), where, experts, b, n, m,
+                                                  _dev(dw, dw_dtype, 3), _SB_DTYPE[dw_dtype], _ptr(ws), ws.numel(), _stream()))
+    return dw
+
+
+# ---- layer norm ------------------------------------------------------------------------------------------------------
+
+def _rows_dtype(x):
+    if x.dtype not in (torch.bfloat16, torch.float32):
+        raise SwitchBackError("rows must be bf16 or f32, got %s" % x.dtype)
+    return x.dtype
+
+
+def layer_norm(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None):
+    """Layer norm of the rows of x [rows, cols] (bf16 or f32); gamma, beta f32 [cols] or None.  Returns (y, mean, rstd), the
+    latter f32 [rows], as layer_norm_backward takes them."""
+    lib = _entries()
+    rows, cols = x.shape
+    dtype = _rows_dtype(x)
+    y = _out(y, (rows, cols), dtype, x.device, "y")
+    mean = _out(mean, (rows,), torch.float32, x.device, "mean")
+    rstd = _out(rstd, (rows,), torch.float32, x.device, "rstd")
+    _on_current_device(x, gamma, beta, y, mean, rstd)
+    _check(lib.switchback_layer_norm(_dev(x, dtype, 2), _SB_DTYPE[dtype], _vec(gamma, cols, x.device, "gamma"),
+                                     _vec(beta, cols, x.device, "beta"), eps, rows, cols, _dev(y, dtype, 2),
+                                     _dev(mean, torch.float32), _dev(rstd, torch.float32), _stream()))
+    return y, mean, rstd
+
+
+def layer_norm_backward(dy, x, mean, rstd, gamma=None, affine=True, dx=None, dgamma=None, dbeta=None, ws=None):
+    """Gradients of layer_norm: dx like x, and the sums over all rows dgamma and dbeta, f32 [cols] (None, None with
+    affine=False)."""
+    lib = _entries()
+    rows, cols = x.shape
+    dtype = _rows_dtype(x)
+    _out(dy, (rows, cols), dtype, x.device, "dy")
+    _out(mean, (rows,), torch.float32, x.device, "mean")
+    _out(rstd, (rows,), torch.float32, x.device, "rstd")
+    dx = _out(dx, (rows, cols), dtype, x.device, "dx")
+    if affine:
+        dgamma = _out(dgamma, (cols,), torch.float32, x.device, "dgamma")
+        dbeta = _out(dbeta, (cols,), torch.float32, x.device, "dbeta")
+        ws = _workspace(SB_OP_LAYER_NORM_BACKWARD, rows, cols, 0, x.device) if ws is None else ws
+    elif dgamma is not None or dbeta is not None:
+        raise SwitchBackError("affine=False computes neither dgamma nor dbeta")
+    _on_current_device(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, ws)
+    _check(lib.switchback_layer_norm_backward(
+        _dev(dy, dtype, 2), _dev(x, dtype, 2), _SB_DTYPE[dtype], _dev(mean, torch.float32), _dev(rstd, torch.float32),
+        _vec(gamma, cols, x.device, "gamma"), rows, cols, _dev(dx, dtype, 2), _dev(dgamma, torch.float32, 1) if affine else None,
+        _dev(dbeta, torch.float32, 1) if affine else None, _ptr(ws) if affine else None,
+        ws.numel() * ws.element_size() if affine else 0, _stream()))
+    return dx, dgamma, dbeta
 
 
 # ---- measured ceilings (include/switchback_ceilings.h): measurement aids of the benchmark, not part of the layer -----

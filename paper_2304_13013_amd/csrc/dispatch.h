@@ -19,9 +19,8 @@ inline bool few_tiles(int64_t M, int64_t N, int ncu) {
 // the measured time has a standard deviation of 10 % per split, and the split picked is 0.3 % slower than the best one in
 // the mean.  k is in stages of 128 bytes.  The 32x32 split is for outputs whose 64x64 blocks leave compute units idle;
 // beyond one block per compute unit it fetches too much (734 x 1600, K = 8064: 45 us, the 64x64 splits 29.5).
-inline double direct_product_time(int64_t M, int64_t N, int64_t K, int ncu, int *split) {
+inline double direct_blocks_time(int64_t blocks32, int64_t blocks64, int64_t K, int ncu, int *split) {
     const double k = (double)((K + 127) / 128);
-    const int64_t blocks32 = ((M + 31) / 32) * (N / 32), blocks64 = ((M + 63) / 64) * (N / 64);
     const int64_t rounds32 = (blocks32 + ncu - 1) / ncu, rounds64 = (blocks64 + ncu - 1) / ncu;
     const int64_t rounds64h = (blocks64 + 2 * ncu - 1) / (2 * ncu);
     const double t32 = 1.6 + (double)rounds32 * (0.5 + 0.079 * k);
@@ -29,6 +28,9 @@ inline double direct_product_time(int64_t M, int64_t N, int64_t K, int ncu, int 
     const double t64h = rounds64 <= 1 ? 2.65 + 0.275 * k : (double)rounds64h * (3.35 + 0.45 * k);
     *split = rounds64 <= 1 && t32 <= t64 && t32 <= t64h ? DIRECT_32 : t64 <= t64h ? DIRECT_64 : DIRECT_64H;
     return *split == DIRECT_32 ? t32 : *split == DIRECT_64 ? t64 : t64h;
+}
+inline double direct_product_time(int64_t M, int64_t N, int64_t K, int ncu, int *split) {
+    return direct_blocks_time(((M + 31) / 32) * (N / 32), ((M + 63) / 64) * (N / 64), K, ncu, split);
 }
 
 // Workgroups of the tiled kernel's persistent grid: a multiple of the XCD count, at most `slots` (what the GPU holds at
@@ -70,8 +72,7 @@ inline bool one_stage(int64_t M, int64_t N, int64_t K, int ncu) {
 // best one in the mean.  Four-byte ones, whose stores weigh as much as the product of a short contraction, to 7000 and (float8)
 // 6000 products within 30 % of the best tile: picked / best 1.003 (1.016 without u: 34752 x 192, K = 384 makes 532 tiles of
 // 128x128, two on a few compute units' both workgroups, 17.6 us, 14.0 on 256x256 ones).
-inline double tiled_product_time(TileKind tile, int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes,
-                                 int ncu) {
+inline double tiles_time(TileKind tile, int64_t tiles, int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes, int ncu) {
     struct Fit {
         double launch, boundary, stage, stage_f, store, boundary_u, stage_u;
     };
@@ -83,23 +84,30 @@ inline double tiled_product_time(TileKind tile, int64_t M, int64_t N, int64_t K,
         {{3.80, 0, 0.339, 0.489, 0.036, 1.90, 0.119}, {4.60, 3.60, 0.426, 0.465, 0.012, 0, 0}, {5.15, 6.61, 0.780, 0.807, 0.016, 0, 0}},
         {{3.47, 0, 0.399, 0.432, 0.028, 2.12, 0.056}, {4.54, 3.65, 0.367, 0.459, 0.015, 0, 0}, {4.88, 6.79, 0.641, 0.844, 0.018, 0, 0}}};
     const Fit &fit = fits[out_bytes == 2 ? (int)kind : kind == PRODUCT_F8 ? 4 : 3][tile];
-    const int bm = tile == TILES_128 ? 128 : 256, bn = tile == TILES_256 ? 256 : 128;
     const int slots = tile == TILES_128 ? 2 * ncu : ncu;
-    const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), per_xcd = persistent_grid(tiles, slots) / 8;
+    const int64_t per_xcd = persistent_grid(tiles, slots) / 8;
     const double rounds = (double)(((tiles + 7) / 8 + per_xcd - 1) / per_xcd), unit = per_xcd * 8 > ncu ? 2 * rounds : rounds;
     const double k = (double)((K + 127) / 128 > 1 || tile != TILES_256X128 ? (K + 127) / 128 : 2);
     return fit.launch + rounds * fit.boundary + unit * fit.boundary_u +
            k * (rounds * fit.stage + (double)tiles / slots * fit.stage_f + unit * fit.stage_u) +
            fit.store * 1e-6 * (double)M * (double)N * out_bytes;
 }
+inline double tiled_product_time(TileKind tile, int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes,
+                                 int ncu) {
+    const int bm = tile == TILES_128 ? 128 : 256, bn = tile == TILES_256 ? 256 : 128;
+    return tiles_time(tile, ((M + bm - 1) / bm) * ((N + bn - 1) / bn), M, N, K, kind, out_bytes, ncu);
+}
 
 // The tile with the smallest estimate; the 128x128 ones on equal terms, up to 3 % with two-byte outputs (the wider ones lose 7
 // % on a narrow miss at worst, where they win 4 % in the mean).  Not for a single stage, where a narrow miss goes the other way
 // (6251 x 1408, K = 128: 8.1 us on 128x128 tiles, 7.3 on 256x256 ones; 24576 x 320: 8.0 and 7.1).
-inline double best_tiles(int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes, int ncu, TileKind *tile) {
-    double best = (K > 128 && out_bytes == 2 ? 0.97 : 1.0) * tiled_product_time(TILES_128, M, N, K, kind, out_bytes, ncu);
-    *tile = TILES_128;
-    for (int i = TILES_128 + 1; i < TILE_KINDS; ++i) {
+// narrowest: the products with a scale for each block have no 128x128 tiles.
+inline double best_tiles(int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes, int ncu, TileKind *tile,
+                         TileKind narrowest = TILES_128) {
+    double best = (narrowest == TILES_128 && K > 128 && out_bytes == 2 ? 0.97 : 1.0) *
+                  tiled_product_time(narrowest, M, N, K, kind, out_bytes, ncu);
+    *tile = narrowest;
+    for (int i = narrowest + 1; i < TILE_KINDS; ++i) {
         const double t = tiled_product_time((TileKind)i, M, N, K, kind, out_bytes, ncu);
         if (t < best) {
             best = t;
@@ -140,10 +148,11 @@ struct ProductPlan {
 // us on 128x128, 256x128 and 256x256 tiles alone / so: 6304 x 768, K = 3072 24.1, 19.9, 31.3 / 20.1; 8000 x 1024, K = 4096 37.5,
 // 29.9, 43.1 / 29.7; 11237 x 2880, K = 1088 49.8, 39.2, 46.4 / 39.4; 30000 x 1280, K = 4096 169, 130, 134 / 124 (whole rounds);
 // 16448 x 1024, K = 4096 87.5, 68.8, 78.9 / 54.0 (last rows).
-inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes, int ncu) {
+inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kind, int out_bytes, int ncu,
+                                TileKind narrowest = TILES_128) {
     ProductPlan plan{0, M, TILES_256, DIRECT_NONE};
     int split = DIRECT_NONE;
-    double best = best_tiles(M, N, K, kind, out_bytes, ncu, &plan.rest);
+    double best = best_tiles(M, N, K, kind, out_bytes, ncu, &plan.rest, narrowest);
     if (few_tiles(M, N, ncu)) {
         const int64_t blocks = ((M + 63) / 64) * (N / 64);
         if (blocks > 2 * (int64_t)ncu) return plan;
@@ -172,8 +181,45 @@ inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kin
     if (whole > 0 && whole < full) {
         TileKind rest;
         const double t = tiled_product_time(TILES_256, whole * 256, N, K, kind, out_bytes, ncu) +
-                         best_tiles(M - whole * 256, N, K, kind, out_bytes, ncu, &rest);
+                         best_tiles(M - whole * 256, N, K, kind, out_bytes, ncu, &rest, narrowest);
         if (t < 0.95 * best) plan = ProductPlan{whole * 256, M, rest, DIRECT_NONE};
+    }
+    return plan;
+}
+
+// A float8 product by experts: `rest` tiles or, unless it is DIRECT_NONE, the small-product kernel with `split`, `runs` workgroups
+// for the row blocks of an expert and a column block.  How the rows fall on experts is known on the GPU alone; the estimates
+// take a row block cut short per expert, or one block each where there are fewer rows than that.
+//
+// The estimates are those of the plain products, and the weights' way from memory at 5.2 TB/s, which the small-product kernel
+// reaches (256 rows, 8 experts of 4096 x 4096: 25.5 us, 40.5 on tiles) and which the tiles hide in part (1000 rows, 64 experts
+// of 2048 x 2048: 41.8 / 70.4; 30000 rows, 64 experts of 2048 x 1024: 82 on tiles, 75 by the plain estimate).  Twice the row blocks of an even share: experts with more rows than others find workgroups for them (2000 rows,
+// 16 experts of 4096 x 1024: 30.6 / 29.6 us; 1000 rows, 8 of 2048 x 2048: 18.4 / 16.9).
+struct ExpertProductPlan {
+    TileKind rest;
+    int split, runs;
+};
+inline ExpertProductPlan plan_expert_product(int64_t M, int64_t N, int64_t K, int64_t experts, int out_bytes, int ncu) {
+    const int64_t used = experts < M ? experts : M;
+    auto row_blocks = [&](int64_t rows) {
+        const int64_t even = (M + rows / 2 * used + rows - 1) / rows;
+        return even > used ? even : used;
+    };
+    ExpertProductPlan plan{TILES_256, DIRECT_NONE, 0};
+    double best = tiles_time(TILES_256, row_blocks(256) * ((N + 255) / 256), M, N, K, PRODUCT_F8, out_bytes, ncu);
+    const double narrow = tiles_time(TILES_256X128, row_blocks(256) * ((N + 127) / 128), M, N, K, PRODUCT_F8, out_bytes, ncu);
+    if (narrow < best) {
+        best = narrow;
+        plan.rest = TILES_256X128;
+    }
+    int split;
+    const double weights = (double)(used * N * K) / 5.2e6;
+    double direct = direct_blocks_time(row_blocks(32) * (N / 32), row_blocks(64) * (N / 64), K, ncu, &split);
+    direct = direct > weights ? direct : weights;
+    if (direct < best + 0.4 * weights) {
+        const int64_t rows = split == DIRECT_32 ? 32 : 64, runs = (2 * ((M + experts - 1) / experts) + rows - 1) / rows;
+        plan.split = split;
+        plan.runs = (int)(runs < 64 ? runs : 64);
     }
     return plan;
 }
@@ -292,6 +338,30 @@ inline WeightGradPlan plan_weight_gradient_in(int64_t b, int64_t n, int64_t m, i
 inline WeightGradPlan plan_weight_gradient(int64_t b, int64_t n, int64_t m, int ncu) {
     const bool narrow = b <= (int64_t)1 << 30 && n <= (int64_t)1 << 18 && m <= (int64_t)1 << 18;  // 64 splits of 2^22 tiles
     return narrow ? plan_weight_gradient_in<int32_t>(b, n, m, ncu) : plan_weight_gradient_in<int64_t>(b, n, m, ncu);
+}
+
+// ---- Weight gradients of experts: the same two kernels, an item for every tile and split of every expert's tokens.  How the
+// tokens fall on experts is known on the GPU alone, so the estimates take the mean.
+struct ExpertGradPlan {
+    bool small;  // 128x128 tiles, else 256x256
+    int splits;  // of every expert's tokens
+};
+inline ExpertGradPlan plan_expert_gradient(int64_t b, int64_t n, int64_t m, int64_t experts, int ncu) {
+    ExpertGradPlan plan{true, 1};
+    double best = 0.0;
+    for (int small = 1; small >= 0; --small) {
+        WeightGradTime<int64_t> time(small, (b + experts - 1) / experts, n, m, ncu);
+        time.tiles *= experts;
+        time.mb *= (double)experts;
+        for (int s = 1; s <= 16 && (s == 1 || time.stages >= s * 4); ++s) {
+            const double t = time.of(s);
+            if ((small && s == 1) || t < best) {
+                best = t;
+                plan = ExpertGradPlan{small != 0, s};
+            }
+        }
+    }
+    return plan;
 }
 
 }  // namespace sb

@@ -8,6 +8,7 @@ namespace {
 
 typedef DirectCfg<32, 32, 4> D32;
 typedef DirectCfg<64, 64, 4> D64;
+typedef DirectCfg<64, 64, 2> D64H;
 
 typedef BlockWideCfg<256> W256;
 typedef BlockWideCfg<128> W128;
@@ -26,6 +27,7 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
     }
 #define WAVES_D32
 #define WAVES_D64
+#define WAVES_D64H
 #define WAVES_W256 __attribute__((amdgpu_waves_per_eu(1, 1)))  // one wave per SIMD: all 512 registers are a lane's
 #define WAVES_W128 __attribute__((amdgpu_waves_per_eu(1, 1)))
 // name suffix: format of the token-side operand, then of the weight-side operand (4 = E4M3, 5 = E5M2)
@@ -40,6 +42,7 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
     SB_BLOCK_ENTRY(name##_a5b5_f32, CFG, OUT_F32, 1, 1)
 SB_BLOCK_ENTRIES(gemm_f8b_d32, D32)
 SB_BLOCK_ENTRIES(gemm_f8b_d64, D64)
+SB_BLOCK_ENTRIES(gemm_f8b_d64h, D64H)
 SB_BLOCK_ENTRIES(gemm_f8b_n, W128)
 SB_BLOCK_ENTRIES(gemm_f8b_w, W256)
 #undef SB_BLOCK_ENTRIES
@@ -49,9 +52,11 @@ typedef void (*Kernel)(GemmBlockArgs);
 #define SB_BLOCK_ROW(name)                                                                                          \
     {name##_a4b4_bf16, name##_a4b4_f32, name##_a5b4_bf16, name##_a5b4_f32, name##_a4b5_bf16, name##_a4b5_f32,       \
      name##_a5b5_bf16, name##_a5b5_f32}
-const Kernel kernels[4][8] = {SB_BLOCK_ROW(gemm_f8b_d32), SB_BLOCK_ROW(gemm_f8b_d64), SB_BLOCK_ROW(gemm_f8b_n), SB_BLOCK_ROW(gemm_f8b_w)};
+enum { K_D32, K_D64, K_D64H, K_N, K_W, KERNELS };
+const Kernel kernels[KERNELS][8] = {SB_BLOCK_ROW(gemm_f8b_d32), SB_BLOCK_ROW(gemm_f8b_d64), SB_BLOCK_ROW(gemm_f8b_d64h),
+                                    SB_BLOCK_ROW(gemm_f8b_n), SB_BLOCK_ROW(gemm_f8b_w)};
 #undef SB_BLOCK_ROW
-std::atomic<bool> lds_set[4][8];  // zero-initialized; a racing second set is harmless
+std::atomic<bool> lds_set[KERNELS][8];  // zero-initialized; a racing second set is harmless
 
 hipError_t launch(int row, int which, int grid, int threads, int lds, const GemmBlockArgs &args, hipStream_t stream) {
     const Kernel kernel = kernels[row][which];
@@ -62,6 +67,33 @@ hipError_t launch(int row, int which, int grid, int threads, int lds, const Gemm
     }
     kernel<<<grid, threads, lds, stream>>>(args);
     return hipGetLastError();
+}
+
+// A direct kernel; runs: workgroups for the row blocks of an expert and a column block.
+hipError_t launch_direct(int split, int runs, int which, GemmBlockArgs args, hipStream_t stream) {
+    args.runs = runs;
+    if (split == DIRECT_32)
+        return launch(K_D32, which, args.N / D32::COLS * args.experts * runs, D32::THREADS, BlockDirect<D32>::LDS_BYTES, args, stream);
+    const int grid = args.N / D64::COLS * args.experts * runs;
+    if (split == DIRECT_64) return launch(K_D64, which, grid, D64::THREADS, BlockDirect<D64>::LDS_BYTES, args, stream);
+    return launch(K_D64H, which, grid, D64H::THREADS, BlockDirect<D64H>::LDS_BYTES, args, stream);
+}
+
+// A tiled kernel; tile_rows: at most as many as there are (experts may have fewer).
+hipError_t launch_tiled(TileKind tile, int64_t tile_rows, int which, const GemmBlockArgs &args, hipStream_t stream) {
+    const bool wide = tile == TILES_256;
+    const int grid = persistent_grid(tile_rows * ((args.N + (wide ? 255 : 127)) / (wide ? 256 : 128)), num_compute_units());
+    if (wide) return launch(K_W, which, grid, W256::THREADS, W256::LDS_BYTES, args, stream);
+    return launch(K_N, which, grid, W128::THREADS, W128::LDS_BYTES, args, stream);
+}
+
+// Rows [first, end) of a product without experts.
+GemmBlockArgs rows_of(GemmBlockArgs a, int64_t first, int64_t end, int64_t out_bytes) {
+    a.a += first * a.K;
+    a.sa += first * a.sa_dwords * 4;
+    a.out = static_cast<char *>(a.out) + first * a.N * out_bytes;
+    a.M = (int)(end - first);
+    return a;
 }
 
 }  // namespace
@@ -81,22 +113,28 @@ hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *sca
     args.K = (int)K;
     args.sa_dwords = (int)((K / 128 + 3) / 4);
     args.experts = (int)experts;
+    args.runs = 0;
     const int which = (fmt_b ? 4 : 0) + (fmt_a ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);
-    const int64_t per_expert = (M + experts - 1) / experts;  // rows, in the mean
-    if (per_expert <= 32) {
-        args.runs = 1;
-        return launch(0, which, (int)(N / D32::COLS * experts), D32::THREADS, BlockDirect<D32>::LDS_BYTES, args, stream);
+    const int ncu = num_compute_units(), out_bytes = out_dtype == SB_BF16 ? 2 : 4;
+    if (offsets != nullptr) {
+        const ExpertProductPlan plan = plan_expert_product(M, N, K, experts, out_bytes, ncu);
+        if (plan.split != DIRECT_NONE) return launch_direct(plan.split, plan.runs, which, args, stream);
+        return launch_tiled(plan.rest, M / 256 + experts, which, args, stream);
     }
-    const int64_t tile_rows = offsets == nullptr ? (M + 255) / 256 : M / 256 + experts;  // at most
-    if (tile_rows * ((N + 255) / 256) * 2 > num_compute_units()) {
-        args.runs = 0;
-        const int wide = tile_rows * ((N + 255) / 256) >= num_compute_units() ? 1 : 0;
-        const int grid = persistent_grid(tile_rows * ((N + 255) / 256) * (wide ? 1 : 2), num_compute_units());
-        return launch(2 + wide, which, grid, 256, wide ? W256::LDS_BYTES : W128::LDS_BYTES, args, stream);
+    const ProductPlan plan = plan_product(M, N, K, PRODUCT_F8, out_bytes, ncu, TILES_256X128);
+    if (plan.first_rows > 0) {
+        const hipError_t e = launch_tiled(TILES_256, plan.first_rows / 256, which, rows_of(args, 0, plan.first_rows, out_bytes), stream);
+        if (e != hipSuccess) return e;
     }
-    const int64_t runs = (per_expert + 63) / 64;
-    args.runs = (int)(runs < 64 ? runs : 64);
-    return launch(1, which, (int)(N / D64::COLS * experts * args.runs), D64::THREADS, BlockDirect<D64>::LDS_BYTES, args, stream);
+    if (plan.tile_rows > plan.first_rows) {
+        const hipError_t e = launch_tiled(plan.rest, (plan.tile_rows - plan.first_rows + 255) / 256, which,
+                                          rows_of(args, plan.first_rows, plan.tile_rows, out_bytes), stream);
+        if (e != hipSuccess) return e;
+    }
+    if (plan.split == DIRECT_NONE) return hipSuccess;
+    const int64_t rows = plan.split == DIRECT_32 ? 32 : 64;
+    return launch_direct(plan.split, (int)((M - plan.tile_rows + rows - 1) / rows), which, rows_of(args, plan.tile_rows, M, out_bytes),
+                         stream);
 }
 
 }  // namespace sb

@@ -78,10 +78,7 @@ hipError_t launch_gemm_bf16_tn(const WeightGradPlan &plan, const void *dy, const
                                sb_dtype dw_dtype, void *ws, hipStream_t stream);
 
 // The same with a gradient per expert: rows offsets[e] .. offsets[e + 1] - 1 (device) of dy and x give dw[e]; dw [experts,m,n].
-struct ExpertGradPlan {
-    bool small;  // 128x128 tiles, else 256x256
-    int splits;
-};
+struct ExpertGradPlan;
 ExpertGradPlan plan_gemm_bf16_tn_experts(int64_t b, int64_t n, int64_t m, int64_t experts);
 size_t gemm_bf16_tn_experts_workspace_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts);
 hipError_t launch_gemm_bf16_tn_experts(const ExpertGradPlan &plan, const void *dy, const void *x, const int32_t *offsets, int64_t experts,

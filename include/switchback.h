@@ -231,8 +231,8 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  * byte 0.  Scale bytes are 0 .. 247.
  *
  * Layouts.  Code rows are whole blocks: K = the row's length rounded up to a multiple of 128, zero codes behind its end.
- * Row scales: [rows, S] bytes with S = K / 128 rounded up to a multiple of 4, 0 behind the last block.  Weight scales:
- * [ceil(m / 128), K / 128] bytes.  All are 16-byte aligned.
+ * Row scales: [S, rows, 4] bytes with S = ceil(K / 512): byte q of row i in part s belongs to block 4 s + q of the row, 0 behind
+ * the last block.  Weight scales: [ceil(m / 128), K / 128] bytes.  All are 16-byte aligned.
  *
  * Experts.  With offsets == NULL there is one weight (experts == 1) and it goes with all rows.  Otherwise weights, codes,
  * scales and weight gradients are [experts, ...] and `offsets` is a device array of experts + 1 non-decreasing int32 row
@@ -241,14 +241,14 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  * call's kernels run, not on the host, and clamped to 0 .. b: others than documented give unspecified values, never a fault.
  * 1 <= experts <= 1024.
  *
- * switchback_quantize_rowwise_f8_block: x [rows,cols] bf16 -> codes [rows,K], scales [rows,S].  cols % 8 == 0, cols <= 131072.
+ * switchback_quantize_rowwise_f8_block: x [rows,cols] bf16 -> codes [rows,K], scales [S,rows,4].  cols % 8 == 0, cols <= 131072.
  * switchback_quantize_weight_f8_block: w [experts,m,n] bf16 -> codes [experts,m,K(n)], scales [experts,ceil(m/128),K(n)/128]
  *   and, unless NULL, the transpose: codes_t [experts,n,K(m)], scales_t [experts,ceil(n/128),K(m)/128].  m % 64 == 0,
  *   n % 64 == 0.
  * switchback_matmul_f8_block: out[i,j] = sum_kb 2^(ea[i,kb] + eb[j/128,kb]) sum_{k in kb} value(aq[i,k]) value(bq[e,j,k]), e the
  *   expert of row i; binary32 accumulation (order unspecified but deterministic; it may depend on the row's place, and the
  *   matrix instruction drops what lies 2^13 below the largest of eight neighbouring products), rounded to nearest even
- *   when SB_BF16.  aq [M,K], scales_a [M,S], bq [experts,N,K], scales_b [experts,ceil(N/128),K/128]; out [M,N], SB_BF16 or
+ *   when SB_BF16.  aq [M,K], scales_a [S,M,4], bq [experts,N,K], scales_b [experts,ceil(N/128),K/128]; out [M,N], SB_BF16 or
  *   SB_F32.  K % 128 == 0, N % 64 == 0, K, N <= 131072, (M + 256) * max(K, N) * 2 < 2^32, (N + 256) * K < 2^32.
  * switchback_linear_f8_block: X [b,n] bf16 quantized by rows in fmt_x, then the product with a weight's codes wq [experts,m,K]
  *   in fmt_w, scales_w: the layer with codes that are kept (serving), and with (dY, codes_t, scales_t, n = m, m = n) its input

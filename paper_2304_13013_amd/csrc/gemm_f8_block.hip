@@ -90,7 +90,8 @@ hipError_t launch_tiled(TileKind tile, int64_t tile_rows, int which, const GemmB
 // Rows [first, end) of a product without experts.
 GemmBlockArgs rows_of(GemmBlockArgs a, int64_t first, int64_t end, int64_t out_bytes) {
     a.a += first * a.K;
-    a.sa += first * a.sa_dwords * 4;
+    a.sa += first * 4;
+    a.sa_bytes -= (int)(first * 4);
     a.out = static_cast<char *>(a.out) + first * a.N * out_bytes;
     a.M = (int)(end - first);
     return a;
@@ -111,7 +112,8 @@ hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *sca
     args.M = (int)M;
     args.N = (int)N;
     args.K = (int)K;
-    args.sa_dwords = (int)((K / 128 + 3) / 4);
+    args.sa_rows = (int)M;
+    args.sa_bytes = (int)(uint32_t)((K / 128 + 3) / 4 * M * 4);
     args.experts = (int)experts;
     args.runs = 0;
     const int which = (fmt_b ? 4 : 0) + (fmt_a ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);

@@ -22,28 +22,35 @@
 namespace sb {
 
 struct GemmBlockArgs {
-    const uint8_t *a, *sa;  // [M,K]; [M, 4 * sa_dwords] bytes, one per block of 128 of a row
+    const uint8_t *a, *sa;  // [M,K]; [ceil(K / 512), sa_rows, 4] bytes: a row's blocks of 128, four to a dword
     const uint8_t *b, *sb;  // [experts,N,K]; [experts, ceil(N / 128), K / 128]
     const int *offsets;     // [experts + 1], or null: one b for all rows
     void *out;              // [M,N]
-    int M, N, K, sa_dwords, experts;
+    int M, N, K, sa_rows, sa_bytes, experts;  // sa_bytes: from sa to the end of the scales, below 2^32
     int runs;               // direct kernel: workgroups that share the row blocks of an expert and a column block
 };
+
+// What all lanes read alike and no kernel writes while this one runs comes through the scalar cache: a vector load would have to
+// be waited for behind all requests before it.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T *from) {
+    typedef const T __attribute__((address_space(4))) constant;
+    return *reinterpret_cast<constant *>(reinterpret_cast<uintptr_t>(from));
+}
 
 // Rows of an expert: [first, end).
 __device__ __forceinline__ void expert_rows(const GemmBlockArgs &p, int e, int *first, int *end) {
     *first = 0;
     *end = p.M;
     if (p.offsets != nullptr) {
-        *first = min(max(p.offsets[e], 0), p.M);
-        *end = min(max(p.offsets[e + 1], *first), p.M);
+        *first = min(max(uniform_load(p.offsets + e), 0), p.M);
+        *end = min(max(uniform_load(p.offsets + e + 1), *first), p.M);
     }
 }
 
-// Byte i of an array that starts at a multiple of 4, the same for all lanes: through the scalar cache, as part of its dword.
+// Byte i of an array that starts at a multiple of 4, as part of its dword.
 __device__ __forceinline__ unsigned uniform_byte(const uint8_t *bytes, int64_t i) {
-    typedef const unsigned __attribute__((address_space(4))) constant_dword;
-    const unsigned v = *reinterpret_cast<constant_dword *>(reinterpret_cast<uintptr_t>(bytes) + (uint64_t)(i & ~(int64_t)3));
+    const unsigned v = uniform_load(reinterpret_cast<const unsigned *>(bytes + (i & ~(int64_t)3)));
     return v >> ((unsigned)(i & 3) * 8) & 0xffu;
 }
 
@@ -76,7 +83,7 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
     const __amdgpu_buffer_rsrc_t rsrc_a =
         __builtin_amdgcn_make_buffer_rsrc((void *)p.a, 0, (unsigned)((size_t)p.M * (size_t)p.K), 0x00020000);
     const __amdgpu_buffer_rsrc_t rsrc_sa =
-        __builtin_amdgcn_make_buffer_rsrc((void *)p.sa, 0, (unsigned)((size_t)p.M * p.sa_dwords * 4), 0x00020000);
+        __builtin_amdgcn_make_buffer_rsrc((void *)p.sa, 0, (unsigned)p.sa_bytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t rsrc_b = __builtin_amdgcn_make_buffer_rsrc(
         (void *)(p.b + (int64_t)expert * p.N * p.K), 0, (unsigned)((size_t)p.N * (size_t)p.K), 0x00020000);
     const int64_t sb_row = ((int64_t)expert * ((p.N + 127) / 128) + n0 / 128) * KB;
@@ -89,7 +96,7 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
     unsigned char *ring = smem + wave * D::WAVE_BYTES;
     const unsigned ring_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring;
     const unsigned req_step = 8u * (unsigned)p.K;
-    const unsigned voff_scale = lane < C::ROWS ? (unsigned)lane * (unsigned)p.sa_dwords * 4 : 0xfffffff0u;
+    const unsigned voff_scale = lane < C::ROWS ? (unsigned)lane * 4 : 0xfffffff0u;
 
     int frag_off[4];
 #pragma unroll
@@ -108,7 +115,7 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, (lds_void *)(dst + C::ROWS * C::BK + r * 1024), 16, voff[r & 1],
                                                          (unsigned)n0 * (unsigned)p.K + (unsigned)r * req_step + k0, 0, 0);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_sa, (lds_void *)(dst + C::STAGE_BYTES), 4, voff_scale,
-                                                     ((unsigned)m0 * (unsigned)p.sa_dwords + ((unsigned)(s0 + i) >> 2)) * 4, 0, 0);
+                                                     ((unsigned)m0 + ((unsigned)(s0 + i) >> 2) * (unsigned)p.sa_rows) * 4, 0, 0);
         };
         v16f acc[C::RB][C::CB];
 #pragma unroll

@@ -5,9 +5,11 @@
 // and fragment reads spread between the matrix instructions, accumulators named in the text, a tile's epilogue under the
 // first half stage of the next one.  What differs:
 //   * A stage is one block of k, so a fragment has one scale per stage.  Token side: the four scale bytes of four blocks are
-//     one dword per row, requested into LDS with every stage (one request of 64 rows a wave) and read with the stage's first
-//     fragments; the stage's byte is shifted down once.  Weight side: a wave's 128 (or 64) columns lie in one block of the
-//     weight, whose byte comes through the scalar cache half a stage ahead.  The matrix instruction takes both as they are.
+//     one dword per row, requested into LDS with every stage (one request of 64 rows a wave), read before the next stage's
+//     first fragments and shifted to the stage's byte where the matrix instructions have done with the register.  Weight
+//     side: a wave's 128 (or 64) columns lie in one block of the weight, whose byte comes through the scalar cache a stage
+//     ahead.  The matrix instruction takes both as they are, at the rate of the plain one (3.86 PFLOP/s from registers on
+//     codes of normal data, 3.89 without scales).
 //   * Tiles belong to experts.  The tile rows of all experts are numbered through; a lane keeps the number of tile rows before
 //     its share of the experts (offsets are read once, when the kernel starts), so that the expert of a tile row is a ballot.
 //     A tile's rows start where its expert's do: the last one of an expert is cut short by the output's bounds check.
@@ -57,8 +59,7 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
         for (int i = 0; i < share; ++i) {
             const int e = lane * share + i;
             if (e < p.experts) {
-                int first, end;
-                expert_rows(p, e, &first, &end);
+                const int first = min(max(p.offsets[e], 0), p.M), end = min(max(p.offsets[e + 1], first), p.M);
                 mine += (end - first + C::BM - 1) / C::BM;
             }
         }
@@ -109,7 +110,6 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     unsigned voff[2];
 #pragma unroll
     for (int v = 0; v < 2; ++v) voff[v] = (unsigned)l_row * p.K + (((lane ^ ((v * 8 + l_row) >> 1)) & 7) << 4);
-    const unsigned voff_scale = (unsigned)(lane * p.sa_dwords) * 4;
     const unsigned req_step = 8u * p.K;
     int l_round = 0, l_left = 0;
     unsigned l_a = 0, l_b = 0, l_s = 0;                      // offsets of the next stage in the operands and the scales
@@ -120,10 +120,10 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
         l_left = t.have ? KT : 1 << 30;
         l_a_bytes = t.have ? (unsigned)p.M * (unsigned)p.K : 0;
         l_b_bytes = t.have ? (unsigned)p.N * (unsigned)p.K : 0;
-        l_s_bytes = t.have ? (unsigned)p.M * (unsigned)p.sa_dwords * 4 : 0;
+        l_s_bytes = t.have ? (unsigned)p.sa_bytes : 0;
         l_a = (unsigned)(t.row + wave * (C::BM / 4)) * (unsigned)p.K;
         l_b = (unsigned)(t.tn * BN + wave * (BN / 4)) * (unsigned)p.K;
-        l_s = (unsigned)(t.row + wave * (C::BM / 4)) * (unsigned)p.sa_dwords * 4;
+        l_s = (unsigned)(t.row + wave * (C::BM / 4)) * 4;
         l_b_base = p.b + (int64_t)t.expert * p.N * p.K;
     };
     auto issue_req = [&](int slot, int i) {
@@ -137,8 +137,8 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     };
     auto issue_scales = [&](int slot) {  // four blocks' bytes per row, of which the stage uses one
         __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)p.sa, 0, l_s_bytes, 0x00020000),
-                                                 (lds_void *)(smem + slot * C::STAGE_BYTES + C::CODE_BYTES + wave * 256), 4, voff_scale,
-                                                 l_s + ((unsigned)(KT - l_left) >> 2) * 4, 0, 0);
+                                                 (lds_void *)(smem + slot * C::STAGE_BYTES + C::CODE_BYTES + wave * 256), 4, lane * 4,
+                                                 l_s + ((unsigned)(KT - l_left) >> 2) * (unsigned)p.sa_rows * 4, 0, 0);
     };
     auto advance = [&]() {
         l_a += C::BK;
@@ -161,7 +161,7 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     const unsigned x_lane = lds_base + wm0 * C::BK + f_off, w_lane = lds_base + C::A_BYTES + wn0 * C::BK + f_off;
     const unsigned s_lane = lds_base + C::CODE_BYTES + (wm0 + f_r) * 4;
     Half xf[2][NBM][2], wf[2][NBN][2];
-    unsigned sx_read[NBM], sx[NBM], sw_read = 0, sw = 0;
+    unsigned sx_read[NBM], sx[NBM], sw_read = 0, sw = 0;  // as read; for the instructions
     auto issue_read = [&](int i, int buf, int slot) {
         constexpr int STEP = 32 * C::BK;
         const int n = i / 2, h = i % 2;  // fragments in the order w0 x0 w1 x1 ..., then the token side's others
@@ -200,12 +200,18 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     int64_t scales_at = weight_scales(t), next_scale = 0;  // of the tile; of the next stage
     sw_read = uniform_byte(p.sb, scales_at);
 #pragma unroll
-    for (int i = 0; i < C::NREADS; ++i) issue_read(i, 0, 0);
-#pragma unroll
     for (int a = 0; a < NBM; ++a) issue_scale_read(a, 0);
+    wait_lds_reads();
+#pragma unroll
+    for (int a = 0; a < NBM; ++a) {
+        asm volatile("" : "+v"(sx_read[a]));
+        sx[a] = sx_read[a];
+    }
+#pragma unroll
+    for (int i = 0; i < C::NREADS; ++i) issue_read(i, 0, 0);
 
     int slot = 0;   // of the stage in work
-    int block = 0;  // of k, that the stage in work is
+    int block = 0;  // of k: the stage that the next half stage 0 works on
     int slack = 0;  // hand-overs whose wait may leave an epilogue's stores outstanding
 
     // ---- Epilogue of the tile that has just been finished.
@@ -308,18 +314,15 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
         if (cur && more) block_barrier();
         pin_frags(cur);
         if (!cur) {
-            const unsigned shift = (unsigned)(block & 3) * 8;
-#pragma unroll
-            for (int a = 0; a < NBM; ++a) {
-                asm volatile("" : "+v"(sx_read[a]));
-                sx[a] = sx_read[a] >> shift;
-            }
             sw = sw_read;
             // Nobody knows of the matrix instructions in the asm: what the vector unit writes is theirs two wait states later.
-#pragma unroll
-            for (int a = 0; a < NBM; ++a) asm volatile("" : "+v"(sx[a]));
-            asm volatile("s_nop 3" : "+v"(sw));
+            asm volatile("s_nop 1" : "+v"(sw));
         }
+        const unsigned shift = (unsigned)(block & 3) * 8;
+        auto next_x_scale = [&](int a) {  // not before the last instruction that uses the scale at hand
+            sx[a] = sx_read[a] >> shift;
+            asm volatile("" : "+v"(sx[a]));
+        };
 #pragma unroll
         for (int idx = 0; idx < C::SLOTS + LAG; ++idx) {
             const int a = idx / NBN, b = idx % NBN;
@@ -338,12 +341,25 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
             if (idx < C::SLOTS)
                 multiply(std::integral_constant<bool, kind == FIRST || kind == FIRST_EPI>(), (a * NBN + b) * 16, wf[cur][b], xf[cur][a], sw, sx[a]);
             if constexpr (more) {
+                // The next stage's scales come before its fragments: four reads behind them they have landed.
+                constexpr int AHEAD = cur ? NBM : 0;
+                if (cur && idx == AHEAD) {
+                    wait_lgkmcnt<AHEAD>();
+#pragma unroll
+                    for (int i = 0; i < NBM; ++i) asm volatile("" : "+v"(sx_read[i]));
+                }
+                if (cur && idx >= AHEAD) {
+#pragma unroll
+                    for (int i = 0; i < NBM - 1; ++i)
+                        if (idx == (NBN * (i + 1) > AHEAD ? NBN * (i + 1) : AHEAD)) next_x_scale(i);
+                }
+                if (!cur && idx == 0) next_x_scale(NBM - 1);
+                if (cur && idx == AHEAD) sw_read = uniform_byte(p.sb, next_scale);
 #pragma unroll
                 for (int i = 2 * idx; i < 2 * idx + 2; ++i) {
-                    if (i < C::NREADS) issue_read(i, nxt, next_slot);
-                    else if (cur && i < C::NREADS + NBM) issue_scale_read(i - C::NREADS, next_slot);
+                    if (i < AHEAD) issue_scale_read(i, next_slot);
+                    else if (i < AHEAD + C::NREADS) issue_read(i - AHEAD, nxt, next_slot);
                 }
-                if (cur && idx == 3) sw_read = uniform_byte(p.sb, next_scale);
                 constexpr int N2 = C::REQ_2ND, N1 = C::REQ - N2;
                 if constexpr (cur == 1) {
                     constexpr int RQ = C::SLOTS / N2;
@@ -386,17 +402,17 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     for (int round = 1;; ++round) {
         for (int kt = 1; kt < KT; ++kt) {
             next_scale = scales_at + kt;
-            period(I1(), KNormal());
             block = kt;
+            period(I1(), KNormal());
             period(I0(), KNormal());
         }
         const Tile next = tile_of(round);
         if (!next.have) break;
         next_scale = scales_at = weight_scales(next);
+        block = 0;
         period(I1(), KNormal());
         epi_begin(t);
         t = next;
-        block = 0;
         period(I0(), KFirstEpi());
     }
     epi_begin(t);

@@ -38,7 +38,7 @@ struct BlockRowsJob {
     const v4u *x;
     int rows, chunks;       // 16-byte chunks of a row
     uint8_t *codes;         // [rows, 128 * blocks]
-    unsigned int *scales;   // [rows, dwords]
+    unsigned int *scales;   // [dwords, rows]
     int blocks, dwords;     // blocks of 128 columns in a row; dwords of scale bytes, one for each 512 columns
     int row_groups, first, count;  // workgroups [first, first + count) of the launch: row_groups for each 512 columns
 };
@@ -69,7 +69,7 @@ __device__ __forceinline__ void quantize_rows(const BlockRowsJob &job, int group
         if (c < job.blocks * 16) reinterpret_cast<v2u *>(job.codes)[(int64_t)(row0 + i) * job.blocks * 16 + c] = codes;
         const unsigned int bytes = __builtin_amdgcn_readlane(s, 0) | __builtin_amdgcn_readlane(s, 16) << 8 |
                                    __builtin_amdgcn_readlane(s, 32) << 16 | __builtin_amdgcn_readlane(s, 48) << 24;
-        if (lane == 0) job.scales[(int64_t)(row0 + i) * job.dwords + part] = bytes;
+        if (lane == 0) job.scales[(int64_t)part * job.rows + row0 + i] = bytes;
     }
 }
 

@@ -597,8 +597,9 @@ def _whole_blocks(cols):
     return -(-cols // 128) * 128
 
 
-def _scale_pitch(cols):
-    return -(-cols // 512) * 4
+def _row_scales(rows, cols):
+    """Shape of the scales of [rows, cols]: a row's blocks four at a time, [parts, rows, 4]."""
+    return -(-cols // 512), rows, 4
 
 
 def _offsets(offsets, lead):
@@ -623,12 +624,12 @@ def _weight_shape(w):
 
 
 def quantize_rowwise_f8_block(x, fmt, codes=None, scales=None):
-    """Blocks of 1 x 128 of a bf16 [rows, cols] tensor -> (codes [rows, K], scales [rows, S]); K is cols rounded up to a
-    multiple of 128, S = K / 128 rounded up to a multiple of 4."""
+    """Blocks of 1 x 128 of a bf16 [rows, cols] tensor -> (codes [rows, K], scales [S, rows, 4]); K is cols rounded up to a
+    multiple of 128, S = ceil(K / 512)."""
     lib = _entries()
     rows, cols = x.shape
     codes = _out(codes, (rows, _whole_blocks(cols)), torch.uint8, x.device, "codes")
-    scales = _out(scales, (rows, _scale_pitch(cols)), torch.uint8, x.device, "scales")
+    scales = _out(scales, _row_scales(rows, cols), torch.uint8, x.device, "scales")
     _on_current_device(x, codes, scales)
     _check(lib.switchback_quantize_rowwise_f8_block(_dev(x, torch.bfloat16, 2), rows, cols, fmt, _dev(codes, torch.uint8),
                                                     _dev(scales, torch.uint8), _stream()))
@@ -671,7 +672,7 @@ def matmul_f8_block(aq, fmt_a, scales_a, bq, fmt_b, scales_b, offsets=None, out=
     if out_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("out must be bf16 or f32")
     out = _out(out, (M, N), out_dtype, aq.device, "out")
-    _out(scales_a, (M, _scale_pitch(K)), torch.uint8, aq.device, "scales_a")
+    _out(scales_a, _row_scales(M, K), torch.uint8, aq.device, "scales_a")
     _on_current_device(aq, scales_a, bq, scales_b, offsets, out)
     _check(lib.switchback_matmul_f8_block(
         _dev(aq, torch.uint8, 2), fmt_a, _dev(scales_a, torch.uint8), _dev(bq, torch.uint8), fmt_b,

@@ -31,6 +31,14 @@ def product_tol(size, k):
     return (7 * 2.0 ** -13 + (k / 64 + 8) * 2.0 ** -23) * size
 
 
+def row_scales(e):
+    """Scale bytes of exponents [rows, blocks] as the kernels take them, [parts, rows, 4], 0 behind the last block."""
+    rows, blocks = e.shape
+    bytes4 = torch.zeros(rows, -(-blocks // 4), 4, dtype=torch.uint8)
+    bytes4.view(rows, -1)[:, :blocks] = e + 127
+    return bytes4.transpose(0, 1).contiguous()
+
+
 def edge_rows(x):
     """Rows (or parts of them) where a scale or a rounding can go wrong."""
     for i in range(min(x.shape[0], 9)):
@@ -69,9 +77,8 @@ def test_row_codes(rows, cols, fmt):
     x = edge_rows((torch.randn(rows, cols, generator=gen) * 3.0).bfloat16())
     codes, scales = sb.quantize_rowwise_f8_block(x.to(DEV), fmt)
     want, e = ref.quantize_rows(x, fmt)
-    assert codes.shape == want.shape and scales.shape == (rows, -(-cols // 512) * 4)
-    assert torch.equal(ref.decode(codes, fmt), want)
-    assert torch.equal(scales.cpu()[:, :e.shape[1]].long(), e + 127) and not scales.cpu()[:, e.shape[1]:].any()
+    assert codes.shape == want.shape
+    assert torch.equal(ref.decode(codes, fmt), want) and torch.equal(scales.cpu(), row_scales(e))
 
 
 @FMT
@@ -108,7 +115,13 @@ def random_offsets(b, experts, gen, first=0, rest=0):
 PRODUCTS = [(1, 64, 128, 0, 0, 0), (31, 192, 384, 0, 0, 0), (65, 64, 640, 0, 0, 0), (300, 256, 1152, 0, 0, 0), (513, 320, 128, 0, 0, 0),
             (1100, 576, 256, 0, 0, 0), (2500, 1088, 512, 0, 0, 0), (700, 4160, 384, 0, 0, 0), (1, 128, 128, 3, 0, 0), (5, 64, 256, 8, 0, 0), (40, 192, 384, 4, 1, 2),
             (333, 128, 640, 5, 0, 0), (1000, 320, 128, 7, 3, 57), (900, 1088, 512, 2, 0, 0), (1500, 640, 256, 33, 0, 100),
-            (64, 64, 1152, 100, 0, 0), (3000, 576, 384, 6, 0, 11), (200, 64, 128, 1024, 0, 0), (5000, 2624, 256, 9, 0, 0)]
+            (64, 64, 1152, 100, 0, 0), (3000, 576, 384, 6, 0, 11), (200, 64, 128, 1024, 0, 0), (5000, 2624, 256, 9, 0, 0),
+            # plain: whole 256x256 tiles and the last rows apart; tiles of both kinds; 256x128; 256x256; 64x64 blocks of two waves
+            (16406, 832, 256, 0, 0, 0), (16665, 960, 640, 0, 0, 0), (644, 3008, 128, 0, 0, 0), (1003, 4096, 1152, 0, 0, 0), (16406, 448, 128, 0, 0, 0),
+            (4011, 2880, 1152, 0, 0, 0), (200, 2368, 128, 0, 0, 0),
+            # by experts: 64x64 blocks of four and of two waves, 256x128 and 256x256 tiles, more than 64 experts on tiles
+            (30, 1152, 512, 47, 0, 0), (30, 576, 128, 47, 0, 0), (372, 2752, 128, 11, 0, 0), (2011, 2048, 2048, 8, 0, 0), (5003, 1088, 768, 24, 5, 61),
+            (9000, 1152, 256, 150, 1, 70)]
 
 
 @pytest.mark.parametrize("M,N,K,experts,first,rest", PRODUCTS)
@@ -121,8 +134,7 @@ def test_products_are_exact_where_nothing_is_dropped(M, N, K, experts, first, re
     a, b = pick(M, K).double(), pick(E, N, K).double()
     ea, eb = torch.randint(-2, 3, (M, kb), generator=gen), torch.randint(-2, 3, (E, nb, kb), generator=gen)
     offsets = random_offsets(M, experts, gen, first, rest) if experts else None
-    scales_a = torch.zeros(M, -(-kb // 4) * 4, dtype=torch.uint8)
-    scales_a[:, :kb] = ea + 127
+    scales_a = row_scales(ea)
     weights = torch.stack([ref.weight_values(b[e], eb[e]) for e in range(E)])
     want, _ = ref.product(ref.row_values(a, ea), weights if experts else weights[0], offsets, untouched=-7.0)
     on = lambda t: (t if experts else t[0]).contiguous().to(DEV)
@@ -141,8 +153,7 @@ def test_scales_at_both_ends():
     a, b = torch.ones(3, K), torch.ones(64, K)
     ea = torch.tensor([[-127, -127], [120, -127], [-60, 120]])
     eb = torch.tensor([[0, 120]])
-    scales_a = torch.zeros(3, 4, dtype=torch.uint8)
-    scales_a[:, :2] = ea + 127
+    scales_a = row_scales(ea)
     want, _ = ref.product(ref.row_values(a.double(), ea), ref.weight_values(b.double(), eb))
     out = sb.matmul_f8_block(ref.encode(a, 0).to(DEV), 0, scales_a.to(DEV), ref.encode(b, 0).to(DEV), 0,
                              (eb + 127).to(torch.uint8).to(DEV), out_dtype=torch.float32)

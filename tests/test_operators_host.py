@@ -101,15 +101,15 @@ def test_binding_refuses():
         lambda: sb.layer_norm_backward(bf(4, 64), bf(4, 64), torch.zeros(3), torch.zeros(4)),
         lambda: sb.layer_norm_backward(bf(4, 64), bf(4, 64), torch.zeros(4), torch.zeros(4), affine=False, dgamma=torch.zeros(64)),
         lambda: sb.quantize_rowwise_f8_block(bf(4, 64), 0), lambda: sb.quantize_rowwise_f8_block(bf(4, 64), 0, codes=u8(4, 64)),
-        lambda: sb.quantize_rowwise_f8_block(bf(4, 64), 0, scales=u8(4, 1)), lambda: sb.quantize_weight_f8_block(bf(64), 0),
+        lambda: sb.quantize_rowwise_f8_block(bf(4, 64), 0, scales=u8(4, 4)), lambda: sb.quantize_weight_f8_block(bf(64), 0),
         lambda: sb.quantize_weight_f8_block(bf(64, 64), 0, codes_t=u8(64, 64)), lambda: sb.quantize_weight_f8_block(bf(2, 2, 64, 64), 0),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(64, 256), 0, u8(1, 2)),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(64, 128), 0, u8(1, 1), offsets=where),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(2, 64, 128), 0, u8(2, 1, 1)),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(3, 64, 128), 0, u8(3, 1, 1), offsets=where),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 1), u8(64, 128), 0, u8(1, 1)),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(64, 128), 0, u8(1, 2)),
-        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(64, 128), 0, u8(1, 1), out=torch.zeros(4, 64, dtype=torch.int32)),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(64, 256), 0, u8(1, 2)),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(64, 128), 0, u8(1, 1), offsets=where),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(2, 64, 128), 0, u8(2, 1, 1)),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(3, 64, 128), 0, u8(3, 1, 1), offsets=where),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(4, 4), u8(64, 128), 0, u8(1, 1)),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(64, 128), 0, u8(1, 2)),
+        lambda: sb.matmul_f8_block(u8(4, 128), 0, u8(1, 4, 4), u8(64, 128), 0, u8(1, 1), out=torch.zeros(4, 64, dtype=torch.int32)),
         lambda: sb.linear_f8_block(bf(4, 64), u8(64, 64), u8(1, 1)), lambda: sb.linear_f8_block(bf(4, 64), u8(64, 128), u8(1, 1), y=bf(4, 32)),
         lambda: sb.linear_f8_block(bf(4, 64), u8(64, 128), u8(1, 1), y=torch.zeros(4, 64, dtype=torch.float16)),
         lambda: sb.forward_f8_block(bf(4, 64), bf(64, 128)), lambda: sb.forward_f8_block(bf(4, 64), bf(2, 64, 64), sb.BlockBuffers(4, 64, 64, 2, "cpu")),

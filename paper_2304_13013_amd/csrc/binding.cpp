@@ -111,6 +111,28 @@ PyObject *out(PyObject *self, PyObject *const *args, Py_ssize_t nargs) {
     return call_general(bound(self)->out, args, nargs);
 }
 
+// device_of(tensors or None ..): the GPU that they live on, -1 if none is on any, -2 if they are on several (tensors that are on
+// no GPU do not count).
+PyObject *device_of(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    long at = -1;
+    for (Py_ssize_t i = 0; i < nargs; ++i) {
+        if (args[i] == Py_None) continue;
+        long here;
+        if (THPVariable_Check(args[i])) {
+            const at::Tensor &t = THPVariable_Unpack(args[i]);
+            here = t.defined() && t.is_cuda() ? t.device().index() : -1;
+        } else {
+            PyObject *r = PyObject_CallMethod(args[i], "get_device", nullptr);
+            if (r == nullptr) return nullptr;
+            here = PyLong_AsLong(r);
+            Py_DECREF(r);
+            if (here == -1 && PyErr_Occurred()) return nullptr;
+        }
+        if (here >= 0) at = at == -1 || at == here ? here : -2;
+    }
+    return PyLong_FromLong(at);
+}
+
 // What ctypes takes for these C types: integers (an address is one) modulo the type's range, None for a null pointer, the
 // structure itself for a pointer to it.
 template <class T>
@@ -139,23 +161,24 @@ bool convert(PyObject *o, T &v, PyObject *saved_type) {
 }
 
 // One entry of the C ABI, its argument types taken from its declaration.
-template <class... A, size_t... I>
-PyObject *call_entry(int (*)(A...), const Entry &e, PyObject *saved_type, PyObject *const *args, Py_ssize_t nargs,
+template <class R, class... A, size_t... I>
+PyObject *call_entry(R (*)(A...), const Entry &e, PyObject *saved_type, PyObject *const *args, Py_ssize_t nargs,
                      std::index_sequence<I...>) {
     std::tuple<A...> v{};
     if (nargs != (Py_ssize_t)sizeof...(A) || !(convert(args[I], std::get<I>(v), saved_type) && ...)) {
         PyErr_Clear();
         return call_general(e.general, args, nargs);
     }
-    int status;
+    R result;
     {
         WithoutGil released;
-        status = reinterpret_cast<int (*)(A...)>(e.address)(std::get<I>(v)...);
+        result = reinterpret_cast<R (*)(A...)>(e.address)(std::get<I>(v)...);
     }
-    return PyLong_FromLong(status);
+    if constexpr (std::is_unsigned<R>::value) return PyLong_FromSize_t(result);
+    else return PyLong_FromLong(result);
 }
-template <class... A>
-constexpr std::index_sequence_for<A...> indices_of(int (*)(A...)) {
+template <class R, class... A>
+constexpr std::index_sequence_for<A...> indices_of(R (*)(A...)) {
     return {};
 }
 template <size_t INDEX, class F>
@@ -197,7 +220,9 @@ PyMethodDef bound_methods[] = {SB_METHOD("dev", &dev),
                                SB_ENTRY(forward_f8_block),
                                SB_ENTRY(backward_weight_experts),
                                SB_ENTRY(layer_norm),
-                               SB_ENTRY(layer_norm_backward)};
+                               SB_ENTRY(layer_norm_backward),
+                               SB_ENTRY(workspace_bytes),
+                               SB_ENTRY(backward_weight_experts_workspace_bytes)};
 constexpr size_t ENTRIES = sizeof(bound_methods) / sizeof(bound_methods[0]) - CHECKS;
 
 // bind(dev, out, saved_type, entry) -> {name: built-in function}: the general forms of the checks, the ctypes structure of
@@ -240,7 +265,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     return functions;
 }
 
-PyMethodDef methods[] = {SB_METHOD("bind", &bind), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {SB_METHOD("bind", &bind), SB_METHOD("device_of", &device_of), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -79,10 +79,13 @@ hipError_t launch_direct(int split, int runs, int which, GemmBlockArgs args, hip
     return launch(K_D64H, which, grid, D64H::THREADS, BlockDirect<D64H>::LDS_BYTES, args, stream);
 }
 
-// A tiled kernel; tile_rows: at most as many as there are (experts may have fewer).
+// A tiled kernel; tile_rows: with experts an upper bound, for which the grid is not shrunk to whole rounds (210 tiles of at most
+// 258: 18.5 us on 136 workgroups, 12.5 on 256).
 hipError_t launch_tiled(TileKind tile, int64_t tile_rows, int which, const GemmBlockArgs &args, hipStream_t stream) {
     const bool wide = tile == TILES_256;
-    const int grid = persistent_grid(tile_rows * ((args.N + (wide ? 255 : 127)) / (wide ? 256 : 128)), num_compute_units());
+    const int64_t tiles = tile_rows * ((args.N + (wide ? 255 : 127)) / (wide ? 256 : 128));
+    const int ncu = num_compute_units();
+    const int grid = persistent_grid(args.offsets != nullptr && tiles > ncu ? ncu : tiles, ncu);
     if (wide) return launch(K_W, which, grid, W256::THREADS, W256::LDS_BYTES, args, stream);
     return launch(K_N, which, grid, W128::THREADS, W128::LDS_BYTES, args, stream);
 }

@@ -402,22 +402,32 @@ __global__ __launch_bounds__(256) void layer_norm_column_sums_kernel(const T *__
     mine[cols + c] = db;
 }
 
-// dgamma and dbeta from `parts` partial sums [parts][2][cols]: 32 columns a workgroup, 32 runs of partial sums each, added in
-// order.  Either may be null.
+// dgamma and dbeta from `parts` partial sums [parts][2][cols]: 16 columns a workgroup, whose 64 runs of partial sums are added
+// in order, then the runs in pairs.  Either may be null.  512 x 2560: 6.4 us with 32 columns and runs, a load at a time; 4.1 so.
 __global__ __launch_bounds__(1024) void layer_norm_reduce_kernel(const float *__restrict__ partial, int parts, int cols,
                                                                  float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    __shared__ float runs[32][33];
-    const int i = threadIdx.x & 31, run = threadIdx.x >> 5, total = 2 * cols;
-    const int at = blockIdx.x * 32 + i;
-    const int first = parts * run / 32, end = parts * (run + 1) / 32;
+    constexpr int COLS = 16, RUNS = 1024 / COLS, AT_ONCE = 8;
+    __shared__ float runs[RUNS][COLS + 1];
+    const int i = threadIdx.x % COLS, run = threadIdx.x / COLS, total = 2 * cols;
+    const int at = blockIdx.x * COLS + i;
+    const int first = parts * run / RUNS, end = parts * (run + 1) / RUNS;
     float sum = 0.0f;
-    if (at < total)
-        for (int k = first; k < end; ++k) sum += partial[(int64_t)k * total + at];
-    runs[run][i] = sum;
-    __syncthreads();
-    if (run == 0 && at < total) {
+    if (at < total) {
+        for (int k = first; k < end; k += AT_ONCE) {
+            float v[AT_ONCE];
 #pragma unroll
-        for (int k = 1; k < 32; ++k) sum += runs[k][i];
+            for (int j = 0; j < AT_ONCE; ++j) v[j] = k + j < end ? partial[(int64_t)(k + j) * total + at] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) sum += v[j];
+        }
+    }
+    runs[run][i] = sum;
+#pragma unroll
+    for (int half = RUNS / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (run < half) runs[run][i] = sum = sum + runs[run + half][i];
+    }
+    if (run == 0 && at < total) {
         float *out = at < cols ? dgamma : dbeta;
         if (out != nullptr) out[at < cols ? at : at - cols] = sum;
     }
@@ -500,7 +510,7 @@ hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *
         if (e != hipSuccess) return e;
     }
     if (sums)
-        layer_norm_reduce_kernel<<<(2 * cols + 31) / 32, 1024, 0, stream>>>(partial, rows > 0 ? blocks : 0, cols, dgamma, dbeta);
+        layer_norm_reduce_kernel<<<(2 * cols + 15) / 16, 1024, 0, stream>>>(partial, rows > 0 ? blocks : 0, cols, dgamma, dbeta);
     return hipGetLastError();
 }
 

@@ -139,16 +139,16 @@ def _load_binding():
 
 
 def _bind():
-    global _native, _bound_to, _dev, _out
+    global _native, _bound_to, _dev, _out, _device_of
     lib, binding = load_library(), _load_binding()
     if binding is None:
-        _native, _dev, _out = lib, _dev_general, _out_general
+        _native, _dev, _out, _device_of = lib, _dev_general, _out_general, _device_of_general
     else:
         def entry(name):
             f = getattr(lib, name)
             return ctypes.cast(f, ctypes.c_void_p).value, f
         _native = types.SimpleNamespace(**binding.bind(_dev_general, _out_general, SbSaved, entry))
-        _dev, _out = _native.dev, _native.out
+        _dev, _out, _device_of = _native.dev, _native.out, binding.device_of
     _bound_to = lib
     return _native
 
@@ -201,7 +201,13 @@ def _out_general(t, shape, dtype, device, name):
     return t
 
 
-_dev, _out = _dev_general, _out_general  # until _bind() puts the built-in forms here, which hand on what is not plain
+def _device_of_general(*tensors):
+    """The GPU that these tensors (or None) live on, -1 if none is on any, -2 if they are on several."""
+    at = {t.get_device() for t in tensors if t is not None} - {-1}
+    return -1 if not at else at.pop() if len(at) == 1 else -2
+
+
+_dev, _out, _device_of = _dev_general, _out_general, _device_of_general  # until _bind() puts the built-in forms here, which hand on what is not plain
 
 
 def _check_bufs(bufs, b, n, m):
@@ -217,7 +223,7 @@ def _check_ws(ws, need, name="workspace"):
 
 
 def workspace_bytes(op, b, n, m):
-    return int(load_library().switchback_workspace_bytes(op, b, n, m))
+    return int(_entries().switchback_workspace_bytes(op, b, n, m))
 
 
 def _workspace(op, b, n, m, device):
@@ -586,11 +592,12 @@ def backward_input_f8(dy, bufs, dx=None, dx_dtype=torch.bfloat16, fmt_g=SB_E5M2,
 # rows offsets[e] .. offsets[e + 1] - 1 are expert e's, rows past the last offset no one's, whose outputs stay as they were.
 
 def _on_current_device(*tensors):
-    """The calls below enqueue on the current device's stream: their tensors have to be there (those on no GPU at all, -1, are
-    refused by the other checks)."""
-    at = {t.get_device() for t in tensors if t is not None} - {-1}
-    if at and at != {_current_device()}:
-        raise SwitchBackError("tensors live on GPU %s, the current device is %d" % (sorted(at), _current_device()))
+    """The calls below enqueue on the current device's stream: their tensors have to be there (those on no GPU at all are refused
+    by the other checks)."""
+    at = _device_of(*tensors)
+    if at != -1 and at != _current_device():
+        raise SwitchBackError("tensors live on %s, the current device is %d"
+                              % ("several GPUs" if at < 0 else "GPU %d" % at, _current_device()))
 
 
 def _whole_blocks(cols):
@@ -765,7 +772,7 @@ def backward_input_f8_block(dy, bufs, offsets=None, dx=None, dx_dtype=torch.bflo
 
 
 def _experts_workspace(b, n, m, experts, device):
-    need = int(load_library().switchback_backward_weight_experts_workspace_bytes(b, n, m, experts))
+    need = int(_entries().switchback_backward_weight_experts_workspace_bytes(b, n, m, experts))
     return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
 
 

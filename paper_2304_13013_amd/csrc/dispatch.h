@@ -187,6 +187,10 @@ inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kin
     return plan;
 }
 
+// Whether rows in 16 bit go to the kernel that quantizes them itself, 16 at a time, and reads a weight once for each 16 rows:
+// 16 rows, or four an expert in the mean.
+inline bool plan_few_rows(int64_t M, int64_t experts) { return M <= 16 || (M <= 4 * experts && M <= 1024); }
+
 // A float8 product by experts: `rest` tiles or, unless it is DIRECT_NONE, the small-product kernel with `split`, `runs` workgroups
 // for the row blocks of an expert and a column block.  How the rows fall on experts is known on the GPU alone; the estimates
 // take a row block cut short per expert, or one block each where there are fewer rows than that.

@@ -1,4 +1,5 @@
 // Host-side dispatch of the float8 product with a scale for each block of 128, plain and grouped by expert.
+#include "gemm_f8_block_few_kernel.h"
 #include "gemm_f8_block_wide_kernel.h"
 
 #include <atomic>
@@ -25,36 +26,42 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
     __global__ __launch_bounds__(CFG::THREADS) WAVES_##CFG void name(GemmBlockArgs p) {              \
         Body<CFG, OUT, FA, FB>::run(p);                                                              \
     }
+#define SB_FEW_ENTRY(name, CFG, OUT, FA, FB) \
+    __global__ __launch_bounds__(FewCfg::THREADS) void name(GemmFewArgs p) { gemm_f8_block_few_body<OUT, FA, FB>(p); }
 #define WAVES_D32
 #define WAVES_D64
 #define WAVES_D64H
 #define WAVES_W256 __attribute__((amdgpu_waves_per_eu(1, 1)))  // one wave per SIMD: all 512 registers are a lane's
 #define WAVES_W128 __attribute__((amdgpu_waves_per_eu(1, 1)))
 // name suffix: format of the token-side operand, then of the weight-side operand (4 = E4M3, 5 = E5M2)
-#define SB_BLOCK_ENTRIES(name, CFG)                        \
-    SB_BLOCK_ENTRY(name##_a4b4_bf16, CFG, OUT_BF16, 0, 0)  \
-    SB_BLOCK_ENTRY(name##_a4b4_f32, CFG, OUT_F32, 0, 0)    \
-    SB_BLOCK_ENTRY(name##_a5b4_bf16, CFG, OUT_BF16, 1, 0)  \
-    SB_BLOCK_ENTRY(name##_a5b4_f32, CFG, OUT_F32, 1, 0)    \
-    SB_BLOCK_ENTRY(name##_a4b5_bf16, CFG, OUT_BF16, 0, 1)  \
-    SB_BLOCK_ENTRY(name##_a4b5_f32, CFG, OUT_F32, 0, 1)    \
-    SB_BLOCK_ENTRY(name##_a5b5_bf16, CFG, OUT_BF16, 1, 1)  \
-    SB_BLOCK_ENTRY(name##_a5b5_f32, CFG, OUT_F32, 1, 1)
-SB_BLOCK_ENTRIES(gemm_f8b_d32, D32)
-SB_BLOCK_ENTRIES(gemm_f8b_d64, D64)
-SB_BLOCK_ENTRIES(gemm_f8b_d64h, D64H)
-SB_BLOCK_ENTRIES(gemm_f8b_n, W128)
-SB_BLOCK_ENTRIES(gemm_f8b_w, W256)
+#define SB_BLOCK_ENTRIES(ENTRY, name, CFG)                        \
+    ENTRY(name##_a4b4_bf16, CFG, OUT_BF16, 0, 0)  \
+    ENTRY(name##_a4b4_f32, CFG, OUT_F32, 0, 0)    \
+    ENTRY(name##_a5b4_bf16, CFG, OUT_BF16, 1, 0)  \
+    ENTRY(name##_a5b4_f32, CFG, OUT_F32, 1, 0)    \
+    ENTRY(name##_a4b5_bf16, CFG, OUT_BF16, 0, 1)  \
+    ENTRY(name##_a4b5_f32, CFG, OUT_F32, 0, 1)    \
+    ENTRY(name##_a5b5_bf16, CFG, OUT_BF16, 1, 1)  \
+    ENTRY(name##_a5b5_f32, CFG, OUT_F32, 1, 1)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d32, D32)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d64, D64)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d64h, D64H)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_n, W128)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_w, W256)
+SB_BLOCK_ENTRIES(SB_FEW_ENTRY, gemm_f8b_few, FewCfg)
+#undef SB_FEW_ENTRY
 #undef SB_BLOCK_ENTRIES
 #undef SB_BLOCK_ENTRY
 
 typedef void (*Kernel)(GemmBlockArgs);
+typedef void (*FewKernel)(GemmFewArgs);
 #define SB_BLOCK_ROW(name)                                                                                          \
     {name##_a4b4_bf16, name##_a4b4_f32, name##_a5b4_bf16, name##_a5b4_f32, name##_a4b5_bf16, name##_a4b5_f32,       \
      name##_a5b5_bf16, name##_a5b5_f32}
 enum { K_D32, K_D64, K_D64H, K_N, K_W, KERNELS };
 const Kernel kernels[KERNELS][8] = {SB_BLOCK_ROW(gemm_f8b_d32), SB_BLOCK_ROW(gemm_f8b_d64), SB_BLOCK_ROW(gemm_f8b_d64h),
                                     SB_BLOCK_ROW(gemm_f8b_n), SB_BLOCK_ROW(gemm_f8b_w)};
+const FewKernel few_kernels[8] = SB_BLOCK_ROW(gemm_f8b_few);
 #undef SB_BLOCK_ROW
 std::atomic<bool> lds_set[KERNELS][8];  // zero-initialized; a racing second set is harmless
 
@@ -101,6 +108,37 @@ GemmBlockArgs rows_of(GemmBlockArgs a, int64_t first, int64_t end, int64_t out_b
 }
 
 }  // namespace
+
+bool few_rows(int64_t M, int64_t experts) { return plan_few_rows(M, experts); }
+
+hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, const uint8_t *bq, int fmt_b, const uint8_t *scales_b,
+                                    const int32_t *offsets, int64_t experts, int64_t M, int64_t N, void *out, sb_dtype out_dtype,
+                                    hipStream_t stream) {
+    static std::atomic<bool> few_lds_set[8];
+    GemmFewArgs args;
+    args.a = static_cast<const uint8_t *>(x);
+    args.sa = nullptr;
+    args.b = bq;
+    args.sb = scales_b;
+    args.offsets = offsets;
+    args.out = out;
+    args.M = (int)M;
+    args.N = (int)N;
+    args.K = (int)((cols + 127) / 128 * 128);
+    args.sa_rows = args.sa_bytes = args.runs = 0;
+    args.experts = (int)experts;
+    args.cols = (int)cols;
+    const int which = (fmt_b ? 4 : 0) + (fmt_x ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);
+    const FewKernel kernel = few_kernels[which];
+    if (!few_lds_set[which].load(std::memory_order_acquire)) {
+        const hipError_t e =
+            hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, FewCfg::LDS_BYTES);
+        if (e != hipSuccess) return e;
+        few_lds_set[which].store(true, std::memory_order_release);
+    }
+    kernel<<<(unsigned int)(N / FewCfg::COLS * experts), FewCfg::THREADS, FewCfg::LDS_BYTES, stream>>>(args);
+    return hipGetLastError();
+}
 
 hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *scales_a, const uint8_t *bq, int fmt_b,
                                 const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M, int64_t N, int64_t K,

@@ -10,19 +10,10 @@
 // What bounds it: memory, 2 bytes read and 1 written per element (weights with their transpose 2 and 2).  A wave owns 512
 // columns of a row at a time (1 KiB of input, one dword of scale bytes), four rows in flight; a weight's block is one workgroup's
 // tile, transposed through LDS.  Both jobs of a forward pass are one launch.
-#include "quantize_common.h"
+#include "quantize_block.h"
 
 namespace sb {
 namespace {
-
-// Scale byte for a block's absmax (15 bits of a bf16 pattern).  As a binary32 pattern the magnitude is 1.f * 2^k, and MAX is
-// 1.75 * 2^8 or 1.75 * 2^15: the exponent goes up by one where 1.f > 1.75.
-template <int CODE>
-__device__ __forceinline__ unsigned int block_scale_byte(unsigned int bits15) {
-    const int s = (int)(((bits15 << 16) + 0x1fffffu) >> 23) - (CODE == CODE_E4M3 ? 8 : 15);
-    return s > 0 ? (unsigned int)s : 0u;
-}
-__device__ __forceinline__ float inverse_of_scale_byte(unsigned int s) { return __uint_as_float((254u - s) << 23); }  // s <= 247
 
 // Largest value of 16 neighbouring lanes, in each of them.
 __device__ __forceinline__ unsigned int max_of_16_lanes(unsigned int v) {

@@ -95,6 +95,11 @@ hipError_t launch_quantize_block(const void *x, int64_t rows, int fmt_x, uint8_t
 hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *scales_a, const uint8_t *bq, int fmt_b,
                                 const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M, int64_t N, int64_t K,
                                 void *out, sb_dtype out_dtype, hipStream_t stream);
+// The product with rows in 16 bit that it quantizes itself, x [M,cols]: for few rows.
+bool few_rows(int64_t M, int64_t experts);
+hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, const uint8_t *bq, int fmt_b, const uint8_t *scales_b,
+                                    const int32_t *offsets, int64_t experts, int64_t M, int64_t N, void *out, sb_dtype out_dtype,
+                                    hipStream_t stream);
 
 // Layer norm (layer_norm.hip): x and y bf16 or f32; gamma, beta, mean, rstd may be null where the C ABI allows it.
 hipError_t launch_layer_norm(const void *x, const float *gamma, const float *beta, float eps, int64_t rows, int64_t cols, bool bf16,

@@ -22,7 +22,10 @@ def half_step(dtype):
 
 
 def within(got, want, tol, what):
-    tol = tol + half_step(got.dtype) * (want.abs() + tol) + 1e-45
+    # A rounding: half a step relative to the value, below the smallest normal number half of the smallest subnormal (bf16: 2^-126
+    # has steps of 2^-133).
+    rounding = half_step(got.dtype) * (want.abs() + tol).clamp(min=torch.finfo(got.dtype).smallest_normal)
+    tol = tol + rounding + 1e-45
     off = (got.cpu().double() - want).abs()
     assert torch.isfinite(off).all() and (off <= tol).all(), "%s: off by %g of the tolerance" % (what, float((off / tol).max()))
 
@@ -195,12 +198,48 @@ def test_layer(b, n, m, experts, rest):
         within(dx, want_dx, product_tol(size_dx, m), "dx")
         kept = torch.zeros_like(y)
         sb.linear_f8_block(x.to(DEV), bufs.wq, bufs.scales_w, offsets=where, y=kept)
-        assert torch.equal(kept, y)
+        within(kept, want, product_tol(size, n), "y on kept codes")
         dw = (sb.backward_weight_experts(dy.to(DEV), x.to(DEV), where, bufs, dw_dtype=dtype) if experts else
               sb.backward_weight(dy.to(DEV), x.to(DEV), bufs, dw_dtype=dtype)[None])
         for e, rows in enumerate(ref.expert_slices(offsets or [0, b], b)):
             g, v = dy[rows].double().t(), x[rows].double()
             within(dw[e], g @ v, (b / 32 + 64) * 2.0 ** -23 * (g.abs() @ v.abs()), "dw")
+
+
+@pytest.mark.parametrize("b,n,m,experts,rest", [(1, 64, 64, None, 0), (1, 4096, 192, None, 0), (16, 576, 320, None, 0), (17, 576, 320, None, 0), (7, 1088, 64, None, 0),
+                                                (5, 128, 64, 8, 1), (60, 320, 128, 16, 3), (96, 2048, 96 * 2, 24, 0), (64, 192, 64, 16, 0)])
+@FMT
+def test_serving_a_few_rows(b, n, m, experts, rest, fmt):
+    """Rows that the product quantizes itself: codes and scales as those of the quantizer, so that products which lose nothing
+    are equal; rows with zeros, ties, subnormals and the largest values; all rows of 16 experts on one of them."""
+    x, _, w, offsets = layer(b, n, m, experts, rest)
+    edge_rows(x)
+    gen = torch.Generator().manual_seed(4)
+    if experts == 16 and rest == 0:
+        offsets = [0] * 8 + [b] * 9
+    where = torch.tensor(offsets, dtype=torch.int32, device=DEV) if experts else None
+    coded = [ref.quantize_weight(part, E4M3) for part in w]
+    stack = lambda ts: (torch.stack(ts) if experts else ts[0]).contiguous().to(DEV)
+    codes, scales = stack([ref.encode(c, E4M3) for c, _ in coded]), stack([(e + 127).to(torch.uint8) for _, e in coded])
+    values = torch.stack([ref.weight_values(c, e)[:, :n] for c, e in coded])
+    xv = ref.row_values(*ref.quantize_rows(x, fmt))[:, :n]
+    want, size = ref.product(xv, values if experts else values[0], offsets, untouched=3.0)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = torch.full((b, m), 3.0, dtype=dtype, device=DEV)
+        sb.linear_f8_block(x.to(DEV), codes, scales, offsets=where, fmt_x=fmt, y=y)
+        fits = size < 1e38  # of the row with the largest value
+        within(y.cpu()[fits], want[fits], product_tol(size[fits], n), "y")
+    # One value a block, the others zero: nothing is dropped, every sum is exact.
+    x = torch.zeros(b, n)
+    for i in range(b):
+        for k in range(0, n, 128):
+            x[i, k + int(torch.randint(0, min(128, n - k), (1,), generator=gen))] = (-1.0) ** i * 2.0 ** int(torch.randint(-8, 8, (1,), generator=gen))
+    ones = torch.ones(experts or 1, m, -(-n // 128) * 128)
+    w_codes = ref.encode(ones, E4M3).to(DEV)
+    exact, _ = ref.product(x.double(), torch.ones(experts, m, n, dtype=torch.float64) if experts else torch.ones(m, n, dtype=torch.float64), offsets)
+    y = torch.zeros(b, m, device=DEV)
+    sb.linear_f8_block(x.bfloat16().to(DEV), w_codes if experts else w_codes[0], torch.full_like(scales, 127), offsets=where, fmt_x=fmt, y=y)
+    assert torch.equal(y.cpu(), exact.float())
 
 
 @pytest.mark.parametrize("b,n,m,experts", [(1, 64, 64, 1), (3, 64, 128, 3), (1000, 128, 64, 2), (5000, 320, 192, 3), (3001, 1088, 576, 9),

@@ -221,20 +221,67 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
     }
 }
 
-// SUMS: the rows' terms of dgamma and dbeta are added up and left in partial[blockIdx.x][2][cols].  gamma lies in LDS, four
+// dgamma and dbeta of 16 columns by a workgroup of `threads`: runs of rows in turn, then the runs in pairs.
+template <class T, int THREADS>
+__device__ __forceinline__ void column_sums(const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean,
+                                            const float *__restrict__ rstd, int rows, int cols, int block, float *__restrict__ dgamma,
+                                            float *__restrict__ dbeta) {
+    constexpr int COLS = 16, RUNS = THREADS / COLS, AT_ONCE = 8;
+    __shared__ float runs[2][RUNS][COLS + 1];
+    const int i = threadIdx.x % COLS, run = threadIdx.x / COLS, c = block * COLS + i;
+    float s[2] = {0.0f, 0.0f};
+    if (c < cols)
+        for (int row = run; row < rows; row += RUNS * AT_ONCE) {
+            float d[AT_ONCE], h[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const int at = min(row + j * RUNS, rows - 1);
+                d[j] = widen(dy[(int64_t)at * cols + c]);
+                h[j] = (widen(x[(int64_t)at * cols + c]) - mean[at]) * rstd[at];
+            }
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j)
+                if (row + j * RUNS < rows) {
+                    s[0] = fmaf(d[j], h[j], s[0]);
+                    s[1] += d[j];
+                }
+        }
+    runs[0][run][i] = s[0];
+    runs[1][run][i] = s[1];
+#pragma unroll
+    for (int half = RUNS / 2; half > 0; half >>= 1) {
+        __syncthreads();
+        if (run < half)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) runs[k][run][i] = s[k] = s[k] + runs[k][run + half][i];
+    }
+    if (run == 0 && c < cols) {
+        if (dgamma != nullptr) dgamma[c] = s[0];
+        if (dbeta != nullptr) dbeta[c] = s[1];
+    }
+}
+
+// SUMS: the rows' terms of dgamma and dbeta are added up and left in partial[blockIdx.x][2][cols].  Without, workgroups from
+// row_blocks on form the sums of 16 columns each from the rows themselves: for few rows, which lie in L2 and are read twice sooner
+// than a second launch starts.  gamma lies in LDS, four
 // consecutive elements of a lane at a time and lanes side by side: in registers, next to the sums and two rows, it would
 // leave one wave per SIMD.
 template <class T, int V, int P, int WAVES, bool SUMS>
 __global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean, const float *__restrict__ rstd,
-    const float *__restrict__ gamma, int64_t rows, int cols, T *__restrict__ dx, float *__restrict__ partial) {
+    const float *__restrict__ gamma, int64_t rows, int cols, T *__restrict__ dx, float *__restrict__ partial, int row_blocks,
+    float *__restrict__ dgamma, float *__restrict__ dbeta) {
     typedef Group<WAVES> G;
+    if (!SUMS && (int)blockIdx.x >= row_blocks) {
+        column_sums<T, G::THREADS>(dy, x, mean, rstd, (int)rows, cols, (int)blockIdx.x - row_blocks, dgamma, dbeta);
+        return;
+    }
     constexpr int Q = V < 4 ? V : 4;
     typedef float Quad __attribute__((ext_vector_type(Q)));
     __shared__ float shared[2][2][16];
     __shared__ Quad weights[P][V / Q][G::LANES];
     const int lane = threadIdx.x % G::LANES;
-    const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)gridDim.x * G::PER_BLOCK;
+    const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)(SUMS ? gridDim.x : row_blocks) * G::PER_BLOCK;
     float dg[SUMS ? P : 1][V], db[SUMS ? P : 1][V];
     if (threadIdx.x < G::LANES) {
 #pragma unroll
@@ -478,6 +525,9 @@ hipError_t forward_of(const T *x, const float *gamma, const float *beta, float e
     return hipGetLastError();
 }
 
+// Few rows: the sums over them in the launch of the rows (FEW_US).
+bool sums_in_one_launch(int64_t rows, int cols, bool whole) { return rows > 0 && rows <= 512 && cols <= longest_row(whole); }
+
 // Workgroups of the backward pass, each of which leaves a pair of partial sums.
 int backward_blocks(int64_t rows, int cols, bool whole) {
     if (cols > longest_row(whole)) return kLongParts;
@@ -487,18 +537,18 @@ int backward_blocks(int64_t rows, int cols, bool whole) {
 template <class T, int V>
 hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *rstd, const float *gamma, int64_t rows, int cols,
                        T *dx, float *dgamma, float *dbeta, float *partial, hipStream_t stream) {
-    const bool sums = dgamma != nullptr || dbeta != nullptr;
+    const bool any = dgamma != nullptr || dbeta != nullptr, one_launch = sums_in_one_launch(rows, cols, V > 1), sums = any && !one_launch;
     const int blocks = backward_blocks(rows, cols, V > 1);
     if (rows > 0) {
         const bool fits = with_group<V>(cols, [&](auto pieces, auto waves) {
             constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
             typedef Group<W> G;
             if (sums)
-                layer_norm_backward_kernel<T, V, P, W, true><<<blocks, G::THREADS, 0, stream>>>(dy, x, mean, rstd, gamma, rows,
-                                                                                                cols, dx, partial);
+                layer_norm_backward_kernel<T, V, P, W, true><<<blocks, G::THREADS, 0, stream>>>(
+                    dy, x, mean, rstd, gamma, rows, cols, dx, partial, 0, nullptr, nullptr);
             else
-                layer_norm_backward_kernel<T, V, P, W, false><<<blocks, G::THREADS, 0, stream>>>(dy, x, mean, rstd, gamma, rows,
-                                                                                                 cols, dx, nullptr);
+                layer_norm_backward_kernel<T, V, P, W, false><<<blocks + (any ? (cols + 15) / 16 : 0), G::THREADS, 0, stream>>>(
+                    dy, x, mean, rstd, gamma, rows, cols, dx, nullptr, blocks, dgamma, dbeta);
         });
         if (!fits) {
             layer_norm_backward_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);
@@ -521,7 +571,8 @@ bool whole_pieces(int64_t cols, bool bf16) { return cols % (bf16 ? 8 : 4) == 0; 
 size_t layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows <= 0) return 0;
     // Either type: rows of whole pieces of four elements need not be of whole pieces of eight.
-    const int a = backward_blocks(rows, (int)cols, true), b = backward_blocks(rows, (int)cols, false);
+    const int a = sums_in_one_launch(rows, (int)cols, true) ? 0 : backward_blocks(rows, (int)cols, true);
+    const int b = sums_in_one_launch(rows, (int)cols, false) ? 0 : backward_blocks(rows, (int)cols, false);
     return (size_t)(a > b ? a : b) * 2 * (size_t)cols * sizeof(float);
 }
 

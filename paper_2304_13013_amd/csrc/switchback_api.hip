@@ -530,10 +530,9 @@ int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype
     const bool sums = dgamma != nullptr || dbeta != nullptr;
     if (rows > 0 && (!ok_ptr(dy) || !ok_ptr(x) || !ok_ptr(dx) || mean == nullptr || rstd == nullptr)) return SB_INVALID_ARG;
     if (!aligned16(gamma) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dgamma) || !aligned4(dbeta)) return SB_INVALID_ARG;
-    if (sums && rows > 0) {
-        if (!ok_ptr(ws)) return SB_INVALID_ARG;
-        if (ws_bytes < sb::layer_norm_backward_workspace_bytes(rows, cols)) return SB_WORKSPACE_TOO_SMALL;
-    }
+    const size_t need = sums ? sb::layer_norm_backward_workspace_bytes(rows, cols) : 0;
+    if (need > 0 && !ok_ptr(ws)) return SB_INVALID_ARG;
+    if (ws_bytes < need) return SB_WORKSPACE_TOO_SMALL;
     return from_hip(sb::launch_layer_norm_backward(dy, x, mean, rstd, gamma, rows, cols, dtype == SB_BF16, dx, dgamma, dbeta, ws,
                                                    static_cast<hipStream_t>(stream)));
 }

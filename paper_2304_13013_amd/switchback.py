@@ -835,15 +835,15 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, affine=True, dx=None, dga
     if affine:
         dgamma = _out(dgamma, (cols,), torch.float32, x.device, "dgamma")
         dbeta = _out(dbeta, (cols,), torch.float32, x.device, "dbeta")
-        ws = _workspace(SB_OP_LAYER_NORM_BACKWARD, rows, cols, 0, x.device) if ws is None else ws
+        need = workspace_bytes(SB_OP_LAYER_NORM_BACKWARD, rows, cols, 0)  # none for few rows
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if ws is None and need else ws
     elif dgamma is not None or dbeta is not None:
         raise SwitchBackError("affine=False computes neither dgamma nor dbeta")
     _on_current_device(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, ws)
     _check(lib.switchback_layer_norm_backward(
         _dev(dy, dtype, 2), _dev(x, dtype, 2), _SB_DTYPE[dtype], _dev(mean, torch.float32), _dev(rstd, torch.float32),
         _vec(gamma, cols, x.device, "gamma"), rows, cols, _dev(dx, dtype, 2), _dev(dgamma, torch.float32, 1) if affine else None,
-        _dev(dbeta, torch.float32, 1) if affine else None, _ptr(ws) if affine else None,
-        ws.numel() * ws.element_size() if affine else 0, _stream()))
+        _dev(dbeta, torch.float32, 1) if affine else None, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream()))
     return dx, dgamma, dbeta
 
 

@@ -89,7 +89,7 @@ def test_without_weights(n, dtype):
     check_backward(dy, x, mean.cpu(), rstd.cpu(), None, dx2, dgamma, dbeta)
 
 
-@pytest.mark.parametrize("b,n", [(4099, 320), (20000, 72), (5000, 2304), (3000, 9000), (2500, 1003)])
+@pytest.mark.parametrize("b,n", [(512, 2056), (513, 2056), (512, 9000), (513, 9000), (511, 8200), (512, 1001), (514, 12001), (4099, 320), (20000, 72), (5000, 2304), (3000, 9000), (2500, 1003)])
 def test_many_rows(b, n):
     """More rows than groups that walk them: a group's registers carry sums from row to row."""
     x, dy, gamma, beta = rows_of(b, n, torch.bfloat16, b + n)

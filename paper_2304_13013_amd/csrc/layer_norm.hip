@@ -5,7 +5,7 @@
 //
 // What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences
 // from it (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large).  Rows of up to 2048 columns
-// belong to a wave, up to 8192 to four and up to 16384 to eight; a group walks many rows, holds gamma and beta (or its
+// belong to a wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and beta (or its
 // shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read from
 // L2 again.  Arithmetic is binary32; y and dx are rounded once.
 //
@@ -71,19 +71,21 @@ __device__ __forceinline__ void load_vector(const float *v, int at, float (&out)
     }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
+// A row belongs to a group of LANES lanes: part of a wave, a wave, or a workgroup.
+template <int LANES_>
+struct Group {
+    static constexpr int LANES = LANES_, THREADS = LANES <= 64 ? 256 : LANES, PER_BLOCK = THREADS / LANES;
+};
 
-// Sums of a group of WAVES waves, in every lane of it.  With more than one wave the group is the workgroup; `turn` alternates,
-// so that one barrier does: who writes a buffer again has passed the barrier of the call between.
-template <int WAVES, int N>
+// Sums of a group, in every lane of it.  A group of several waves is the workgroup; `turn` alternates, so that one barrier does:
+// who writes a buffer again has passed the barrier of the call between.
+template <int LANES, int N>
 __device__ __forceinline__ void group_sums(float (&v)[N], float (*shared)[2][16], int turn) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-    if constexpr (WAVES > 1) {
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int off = (LANES < 64 ? LANES : 64) / 2; off > 0; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
+    if constexpr (LANES > 64) {
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) shared[turn][i][threadIdx.x >> 6] = v[i];
@@ -92,23 +94,18 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*shared)[2][16]
         for (int i = 0; i < N; ++i) {
             v[i] = shared[turn][i][0];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) v[i] += shared[turn][i][w];
+            for (int w = 1; w < LANES / 64; ++w) v[i] += shared[turn][i][w];
         }
     }
 }
 
-template <int WAVES>
-struct Group {
-    static constexpr int LANES = 64 * WAVES, THREADS = WAVES == 1 ? 256 : LANES, PER_BLOCK = THREADS / LANES;
-};
-
-// Rows of up to 64 * WAVES * V * P columns; P pieces a lane.  mean and rstd may be null, and gamma and beta.
-template <class T, int V, int P, int WAVES>
-__global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
+// Rows of up to LANES * V * P columns; P pieces a lane.  mean and rstd may be null, and gamma and beta.
+template <class T, int V, int P, int LANES>
+__global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
                                                                             const float *__restrict__ beta, float eps,
                                                                             int64_t rows, int cols, T *__restrict__ y,
                                                                             float *__restrict__ mean, float *__restrict__ rstd) {
-    typedef Group<WAVES> G;
+    typedef Group<LANES> G;
     __shared__ float shared[2][2][16];
     const int lane = threadIdx.x % G::LANES;
     const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)gridDim.x * G::PER_BLOCK;
@@ -134,7 +131,7 @@ __global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_kernel(const
     };
     const float inv = 1.0f / (float)cols;
     if (first < rows) request(first);
-    // All waves of a workgroup make the same number of rounds where they meet at barriers: WAVES > 1 has one row a workgroup.
+    // All waves of a workgroup make the same number of rounds where they meet at barriers: it has one row then.
     for (int64_t row = first; row < rows; row += step) {
         float v[P][V], s[1] = {0.0f};
 #pragma unroll
@@ -145,7 +142,7 @@ __global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_kernel(const
                 s[0] += v[p][e];
             }
         if (row + step < rows) request(row + step);
-        group_sums<WAVES, 1>(s, shared, 0);
+        group_sums<LANES, 1>(s, shared, 0);
         const float mu = s[0] * inv;
         s[0] = 0.0f;
 #pragma unroll
@@ -157,7 +154,7 @@ __global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_kernel(const
                 s[0] = fmaf(v[p][e], v[p][e], s[0]);
             }
         }
-        group_sums<WAVES, 1>(s, shared, 1);
+        group_sums<LANES, 1>(s, shared, 1);
         const float r = 1.0f / sqrtf(s[0] * inv + eps);
         if (lane == 0) {
             if (mean != nullptr) mean[row] = mu;
@@ -190,7 +187,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
 #pragma unroll
             for (int e = 0; e < V; ++e) s[0] += widen(q.e[e]);
         }
-        group_sums<16, 1>(s, shared, 0);
+        group_sums<1024, 1>(s, shared, 0);
         const float mu = s[0] * inv;
         s[0] = 0.0f;
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
@@ -201,7 +198,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
                 s[0] = fmaf(d, d, s[0]);
             }
         }
-        group_sums<16, 1>(s, shared, 1);
+        group_sums<1024, 1>(s, shared, 1);
         const float r = 1.0f / sqrtf(s[0] * inv + eps);
         if (threadIdx.x == 0) {
             if (mean != nullptr) mean[row] = mu;
@@ -266,12 +263,12 @@ __device__ __forceinline__ void column_sums(const T *__restrict__ dy, const T *_
 // than a second launch starts.  gamma lies in LDS, four
 // consecutive elements of a lane at a time and lanes side by side: in registers, next to the sums and two rows, it would
 // leave one wave per SIMD.
-template <class T, int V, int P, int WAVES, bool SUMS>
-__global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_backward_kernel(
+template <class T, int V, int P, int LANES, bool SUMS>
+__global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean, const float *__restrict__ rstd,
     const float *__restrict__ gamma, int64_t rows, int cols, T *__restrict__ dx, float *__restrict__ partial, int row_blocks,
     float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    typedef Group<WAVES> G;
+    typedef Group<LANES> G;
     if (!SUMS && (int)blockIdx.x >= row_blocks) {
         column_sums<T, G::THREADS>(dy, x, mean, rstd, (int)rows, cols, (int)blockIdx.x - row_blocks, dgamma, dbeta);
         return;
@@ -340,7 +337,7 @@ __global__ __launch_bounds__(Group<WAVES>::THREADS) void layer_norm_backward_ker
             }
         }
         if (row + step < rows) request(row + step);
-        group_sums<WAVES, 2>(s, shared, turn);
+        group_sums<LANES, 2>(s, shared, turn);
         const float sa = s[0] * inv, sh = s[1] * inv;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -416,7 +413,7 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T 
                 s[1] = fmaf(a, (widen(q.e[e]) - mu) * r, s[1]);
             }
         }
-        group_sums<16, 2>(s, shared, turn);
+        group_sums<1024, 2>(s, shared, turn);
         const float sa = s[0] * inv, sh = s[1] * inv;
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
             const Piece<T, V> q = load_piece<T, V, false>(xr + c), d = load_piece<T, V, false>(dr + c);
@@ -488,24 +485,31 @@ int walkers(int64_t rows, int per_block, int per_cu) {
     return (int)(need < most ? need : most);
 }
 
-// The group and the pieces for rows of `cols` columns, V elements a piece: calls f(integral constants P, WAVES), or returns
+// The group and the pieces for rows of `cols` columns, V elements a piece: calls f(integral constants P, LANES), or returns
 // false for rows that do not fit.  A lane holds at most 32 elements; eight waves only of whole pieces (the others' 32 addresses
-// would not fit in its registers).
+// would not fit in its registers), parts of a wave too (rows of single elements would be many loads).
 template <int V, class F>
 bool with_group(int cols, F f) {
-    auto go = [&](auto elements, auto waves) {
-        constexpr int E = decltype(elements)::value, W = decltype(waves)::value;
-        if (cols > 64 * W * E) return false;
-        f(std::integral_constant<int, E / V>(), waves);
+    auto go = [&](auto elements, auto lanes) {
+        constexpr int E = decltype(elements)::value, L = decltype(lanes)::value;
+        if (cols > L * E) return false;
+        f(std::integral_constant<int, E / V>(), lanes);
         return true;
     };
-    typedef std::integral_constant<int, 1> W1;
-    typedef std::integral_constant<int, 4> W4;
-    typedef std::integral_constant<int, 8> W8;
-    const bool done = go(std::integral_constant<int, 8>(), W1()) || go(std::integral_constant<int, 16>(), W1()) ||
-                      go(std::integral_constant<int, 24>(), W1()) || go(std::integral_constant<int, 32>(), W1()) ||
-                      go(std::integral_constant<int, 16>(), W4()) || go(std::integral_constant<int, 32>(), W4());
-    if constexpr (V > 1) return done || go(std::integral_constant<int, 32>(), W8());
+    typedef std::integral_constant<int, 8> E8;
+    typedef std::integral_constant<int, 16> E16;
+    typedef std::integral_constant<int, 24> E24;
+    typedef std::integral_constant<int, 32> E32;
+    typedef std::integral_constant<int, 64> Wave;
+    typedef std::integral_constant<int, 256> FourWaves;
+    typedef std::integral_constant<int, 512> EightWaves;
+    if constexpr (V > 1) {
+        if (go(E8(), std::integral_constant<int, 8>()) || go(E8(), std::integral_constant<int, 16>()) || go(E8(), std::integral_constant<int, 32>()))
+            return true;
+    }
+    const bool done = go(E8(), Wave()) || go(E16(), Wave()) || go(E24(), Wave()) || go(E32(), Wave()) || go(E16(), FourWaves()) ||
+                      go(E32(), FourWaves());
+    if constexpr (V > 1) return done || go(E32(), EightWaves());
     return done;
 }
 // Columns of the longest rows that fit.
@@ -514,10 +518,10 @@ int longest_row(bool whole) { return whole ? 16384 : 8192; }
 template <class T, int V>
 hipError_t forward_of(const T *x, const float *gamma, const float *beta, float eps, int64_t rows, int cols, T *y, float *mean,
                       float *rstd, hipStream_t stream) {
-    const bool fits = with_group<V>(cols, [&](auto pieces, auto waves) {
-        constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
-        typedef Group<W> G;
-        layer_norm_kernel<T, V, P, W><<<walkers(rows, G::PER_BLOCK, W == 8 ? 4 : 8), G::THREADS, 0, stream>>>(
+    const bool fits = with_group<V>(cols, [&](auto pieces, auto lanes) {
+        constexpr int P = decltype(pieces)::value, L = decltype(lanes)::value;
+        typedef Group<L> G;
+        layer_norm_kernel<T, V, P, L><<<walkers(rows, G::PER_BLOCK, L == 512 ? 4 : 8), G::THREADS, 0, stream>>>(
             x, gamma, beta, eps, rows, cols, y, mean, rstd);
     });
     if (!fits)
@@ -525,13 +529,27 @@ hipError_t forward_of(const T *x, const float *gamma, const float *beta, float e
     return hipGetLastError();
 }
 
-// Few rows: the sums over them in the launch of the rows (FEW_US).
-bool sums_in_one_launch(int64_t rows, int cols, bool whole) { return rows > 0 && rows <= 512 && cols <= longest_row(whole); }
+// Rows that a workgroup works on at a time, of at most 2048 columns.
+int rows_per_block(int cols, bool whole) { return !whole || cols > 256 ? 4 : cols > 128 ? 8 : cols > 64 ? 16 : 32; }
 
-// Workgroups of the backward pass, each of which leaves a pair of partial sums.
+// Few rows: the sums over them in the launch of the rows, which are read twice (1200 x 768 bf16: 7.6 us, 9.5 in two launches; 600 x
+// 2048 f32 6.5 / 12.2; on the other side 1200 x 4096 f32 22.9 / 22.1, 2500 x 768 bf16 19.7 / 10.8).
+bool sums_in_one_launch(int64_t rows, int cols, bool whole) {
+    return rows > 0 && rows <= 1024 && rows * cols <= 1 << 22 && cols <= longest_row(whole);
+}
+
+// Workgroups of the backward pass, each of which leaves a pair of partial sums: a large part of the traffic where it has few
+// rows.  A workgroup a compute unit for rows of several waves (6000 x 8192 bf16: 68.6 us, 78.4 with two; 5000 x 4096 38.4 / 39.5), of
+// four rows at least (600 x 16384: 41.2 on 128 workgroups, 47.5 on 256); two for shorter ones unless that leaves a group fewer
+// than two rows (32896 x 1280: 50.4, 55.0 with one; 2500 x 2048 f32 27.6 / 21.4).
 int backward_blocks(int64_t rows, int cols, bool whole) {
     if (cols > longest_row(whole)) return kLongParts;
-    return cols > 8192 ? walkers(rows, 1, 1) : cols > 2048 ? walkers(rows, 1, 2) : walkers(rows, 4, 2);
+    if (cols > 2048) {
+        const int64_t four = (rows + 3) / 4;
+        return (int)(four < num_compute_units() ? four : num_compute_units());
+    }
+    const int per_block = rows_per_block(cols, whole);
+    return walkers(rows, per_block, rows >= (int64_t)4 * per_block * num_compute_units() ? 2 : 1);
 }
 
 template <class T, int V>
@@ -540,15 +558,17 @@ hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *
     const bool any = dgamma != nullptr || dbeta != nullptr, one_launch = sums_in_one_launch(rows, cols, V > 1), sums = any && !one_launch;
     const int blocks = backward_blocks(rows, cols, V > 1);
     if (rows > 0) {
-        const bool fits = with_group<V>(cols, [&](auto pieces, auto waves) {
-            constexpr int P = decltype(pieces)::value, W = decltype(waves)::value;
-            typedef Group<W> G;
+        const bool fits = with_group<V>(cols, [&](auto pieces, auto lanes) {
+            constexpr int P = decltype(pieces)::value, L = decltype(lanes)::value;
+            typedef Group<L> G;
             if (sums)
-                layer_norm_backward_kernel<T, V, P, W, true><<<blocks, G::THREADS, 0, stream>>>(
+                layer_norm_backward_kernel<T, V, P, L, true><<<blocks, G::THREADS, 0, stream>>>(
                     dy, x, mean, rstd, gamma, rows, cols, dx, partial, 0, nullptr, nullptr);
-            else
-                layer_norm_backward_kernel<T, V, P, W, false><<<blocks + (any ? (cols + 15) / 16 : 0), G::THREADS, 0, stream>>>(
-                    dy, x, mean, rstd, gamma, rows, cols, dx, nullptr, blocks, dgamma, dbeta);
+            else {
+                const int row_blocks = walkers(rows, G::PER_BLOCK, 4);
+                layer_norm_backward_kernel<T, V, P, L, false><<<row_blocks + (any ? (cols + 15) / 16 : 0), G::THREADS, 0, stream>>>(
+                    dy, x, mean, rstd, gamma, rows, cols, dx, nullptr, row_blocks, dgamma, dbeta);
+            }
         });
         if (!fits) {
             layer_norm_backward_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);

@@ -187,9 +187,22 @@ inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kin
     return plan;
 }
 
-// Whether rows in 16 bit go to the kernel that quantizes them itself, 16 at a time, and reads a weight once for each 16 rows:
-// 16 rows, or four an expert in the mean.
-inline bool plan_few_rows(int64_t M, int64_t experts) { return M <= 16 || (M <= 4 * experts && M <= 1024); }
+// Whether rows in 16 bit go to the kernel that quantizes them itself, 16 at a time, and reads a weight once for each 16 rows: 16
+// rows, or four an expert in the mean; and small products, where the launch of the quantizer would be most of the time.  Two
+// launches / this one (us): 16 rows, 4096 -> 16384 from memory 17.6 / 15.5; 64 rows, 1024 -> 1024 6.3 / 4.0; 512 rows, 1024 ->
+// 256 7.0 / 4.1; 1024 rows, 512 -> 512 7.1 / 5.8; 32 rows, 4096 -> 4096 8.1 / 7.6; 256 rows, 32 experts of 1024 x 1024 11.5 / 8.8; on the
+// other side 64 rows, 4096 -> 4096 9.1 / 11.6; 128 rows, 8192 -> 512 11.5 / 12.1.
+inline bool plan_few_rows(int64_t M, int64_t N, int64_t K, int64_t experts) {
+    if (M <= 16 || (M <= 4 * experts && M <= 1024)) return true;
+    const int64_t used = experts < M ? experts : M, even = experts == 1 ? (M + 15) / 16 : (M + 8 * used + 15) / 16;
+    const int64_t blocks = (even > used ? even : used) * (N / 32);
+    return blocks <= 1024 && K <= 4096 && blocks * K <= 1 << 20;
+}
+// Workgroups that share the row blocks of a weight and 32 of its columns: twice those of an even share, as above.
+inline int plan_few_runs(int64_t M, int64_t experts) {
+    const int64_t runs = (2 * ((M + experts - 1) / experts) + 15) / 16;
+    return (int)(experts == 1 ? (M + 15) / 16 : M <= 4 * experts ? 1 : runs);
+}
 
 // A float8 product by experts: `rest` tiles or, unless it is DIRECT_NONE, the small-product kernel with `split`, `runs` workgroups
 // for the row blocks of an expert and a column block.  How the rows fall on experts is known on the GPU alone; the estimates

@@ -109,7 +109,7 @@ GemmBlockArgs rows_of(GemmBlockArgs a, int64_t first, int64_t end, int64_t out_b
 
 }  // namespace
 
-bool few_rows(int64_t M, int64_t experts) { return plan_few_rows(M, experts); }
+bool few_rows(int64_t M, int64_t N, int64_t K, int64_t experts) { return plan_few_rows(M, N, K, experts); }
 
 hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, const uint8_t *bq, int fmt_b, const uint8_t *scales_b,
                                     const int32_t *offsets, int64_t experts, int64_t M, int64_t N, void *out, sb_dtype out_dtype,
@@ -125,7 +125,8 @@ hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, cons
     args.M = (int)M;
     args.N = (int)N;
     args.K = (int)((cols + 127) / 128 * 128);
-    args.sa_rows = args.sa_bytes = args.runs = 0;
+    args.sa_rows = args.sa_bytes = 0;
+    args.runs = plan_few_runs(M, experts);
     args.experts = (int)experts;
     args.cols = (int)cols;
     const int which = (fmt_b ? 4 : 0) + (fmt_x ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);
@@ -136,7 +137,7 @@ hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, cons
         if (e != hipSuccess) return e;
         few_lds_set[which].store(true, std::memory_order_release);
     }
-    kernel<<<(unsigned int)(N / FewCfg::COLS * experts), FewCfg::THREADS, FewCfg::LDS_BYTES, stream>>>(args);
+    kernel<<<(unsigned int)(N / FewCfg::COLS * experts * args.runs), FewCfg::THREADS, FewCfg::LDS_BYTES, stream>>>(args);
     return hipGetLastError();
 }
 

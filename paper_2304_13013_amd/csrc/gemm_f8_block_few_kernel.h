@@ -11,7 +11,8 @@
 // eight waves where there is a workgroup a compute unit (8 rows, 8192 -> 8192: 13.6 -> 16.5; 16 rows, 16384 -> 4096: 23.7 -> 22.1).
 // v_mfma_scale_f32_16x16x128_f8f6f4 takes a block of k at once: 16 rows, the weight's columns as the first operand, so that a
 // lane owns one row and four columns.  Rows past the last one are not fetched.  More than 16 rows of a weight are worked off 16 at
-// a time, the weight read again: the dispatch sees to it that they are rare.
+// a time, by `runs` workgroups, the weight read again by each: the dispatch sees to it that they are rare, or the product
+// small and the launch most of its time.
 #pragma once
 #include "gemm_f8_block_kernel.h"
 #include "quantize_block.h"
@@ -40,10 +41,11 @@ __device__ __forceinline__ void gemm_f8_block_few_body(const GemmFewArgs &p) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 15, part = lane >> 4;  // of a fragment: part is a quarter of the block of k
-    const int cols = p.N / C::COLS, n0 = (int)blockIdx.x % cols * C::COLS, expert = (int)blockIdx.x / cols;
+    const int cols = p.N / C::COLS, n0 = (int)blockIdx.x % cols * C::COLS, rest = (int)blockIdx.x / cols;
+    const int run = rest % p.runs, expert = rest / p.runs;
     int first, end;
     expert_rows(p, expert, &first, &end);
-    if (first >= end) return;
+    if (first + run * C::ROWS >= end) return;
     const int KB = p.K / C::BK;
     const int s0 = (int)((long long)wave * KB / C::WAVES), s1 = (int)((long long)(wave + 1) * KB / C::WAVES), n = s1 - s0;
 
@@ -56,7 +58,7 @@ __device__ __forceinline__ void gemm_f8_block_few_body(const GemmFewArgs &p) {
     unsigned char *ring = smem + wave * C::WAVE_BYTES;
     const unsigned ring_at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)ring;
 
-    for (int m0 = first; m0 < end; m0 += C::ROWS) {
+    for (int m0 = first + run * C::ROWS; m0 < end; m0 += p.runs * C::ROWS) {
         const int rows = min(end - m0, C::ROWS);
         const __amdgpu_buffer_rsrc_t rsrc_x = __builtin_amdgcn_make_buffer_rsrc(
             (void *)(reinterpret_cast<const unsigned short *>(p.a) + (int64_t)m0 * p.cols), 0, (unsigned)(rows * p.cols * 2), 0x00020000);

@@ -96,7 +96,7 @@ hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *sca
                                 const uint8_t *scales_b, const int32_t *offsets, int64_t experts, int64_t M, int64_t N, int64_t K,
                                 void *out, sb_dtype out_dtype, hipStream_t stream);
 // The product with rows in 16 bit that it quantizes itself, x [M,cols]: for few rows.
-bool few_rows(int64_t M, int64_t experts);
+bool few_rows(int64_t M, int64_t N, int64_t K, int64_t experts);
 hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, const uint8_t *bq, int fmt_b, const uint8_t *scales_b,
                                     const int32_t *offsets, int64_t experts, int64_t M, int64_t N, void *out, sb_dtype out_dtype,
                                     hipStream_t stream);

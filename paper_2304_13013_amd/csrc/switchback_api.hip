@@ -460,7 +460,7 @@ int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint
     if (!ok_ptr(x_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w) || !ok_ptr(y) || !ok_ptr(ws) || !aligned4(offsets)) return SB_INVALID_ARG;
     if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (sb::few_rows(b, experts))
+    if (sb::few_rows(b, m, n, experts))
         return from_hip(sb::launch_gemm_f8_block_few(x_bf16, n, fmt_x, wq, fmt_w, scales_w, offsets, experts, b, m, y, y_dtype, s));
     uint8_t *xq = static_cast<uint8_t *>(ws), *scales_x = xq + row_codes_bytes(b, n);
     const hipError_t e = sb::launch_quantize_rows_block(x_bf16, b, n, fmt_x, xq, scales_x, s);

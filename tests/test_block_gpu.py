@@ -207,7 +207,8 @@ def test_layer(b, n, m, experts, rest):
 
 
 @pytest.mark.parametrize("b,n,m,experts,rest", [(1, 64, 64, None, 0), (1, 4096, 192, None, 0), (16, 576, 320, None, 0), (17, 576, 320, None, 0), (7, 1088, 64, None, 0),
-                                                (5, 128, 64, 8, 1), (60, 320, 128, 16, 3), (96, 2048, 96 * 2, 24, 0), (64, 192, 64, 16, 0)])
+                                                (5, 128, 64, 8, 1), (60, 320, 128, 16, 3), (96, 2048, 96 * 2, 24, 0), (64, 192, 64, 16, 0),
+                                                (100, 1024, 256, None, 0), (500, 576, 192, None, 0), (333, 320, 256, 5, 7), (1000, 128, 64, 3, 0)])
 @FMT
 def test_serving_a_few_rows(b, n, m, experts, rest, fmt):
     """Rows that the product quantizes itself: codes and scales as those of the quantizer, so that products which lose nothing

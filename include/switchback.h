@@ -56,7 +56,7 @@ typedef enum {
     SB_OP_QUANTIZE_COLWISE = 4, /* also the workspace of switchback_backward_input_q; pass rows as m, cols as n */
     SB_OP_STABLE_ADAMW = 5,     /* shape arguments ignored */
     SB_OP_LAYER_NORM_BACKWARD = 6, /* pass rows as b, cols as n */
-    SB_OP_LINEAR_F8_BLOCK = 7   /* pass the layer's input width as n; m ignored */
+    SB_OP_FORWARD_F8_BLOCK = 7  /* m ignored */
 } sb_op;
 
 /* What the forward pass leaves for the backward pass (Algorithm 1 saves X and W in 16 bit and re-quantizes W in
@@ -252,9 +252,11 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  *   SB_F32.  K % 128 == 0, N % 64 == 0, K, N <= 131072, (M + 256) * max(K, N) * 2 < 2^32, (N + 256) * K < 2^32.
  * switchback_linear_f8_block: X [b,n] bf16 quantized by rows in fmt_x, then the product with a weight's codes wq [experts,m,K]
  *   in fmt_w, scales_w: the layer with codes that are kept (serving), and with (dY, codes_t, scales_t, n = m, m = n) its input
- *   gradient.  y [b,m].  ws: SB_OP_LINEAR_F8_BLOCK workspace.
+ *   gradient.  y [b,m].  ws: switchback_linear_f8_block_workspace_bytes(b, n, m, experts) bytes (0 for few rows and small
+ *   products, whose kernel quantizes the rows itself; ws may then be NULL).
  * switchback_forward_f8_block: W [experts,m,n] quantized (into the four code and scale arrays, codes_t and scales_t may be
- *   NULL), then as switchback_linear_f8_block.  b == 0 still quantizes W.  m % 64 == 0, n % 64 == 0; other limits as above.
+ *   NULL) and X, then the product.  ws: SB_OP_FORWARD_F8_BLOCK workspace.  b == 0 still quantizes W.  m % 64 == 0, n % 64 == 0;
+ *   other limits as above.
  * The weight gradient of the plain layer is switchback_backward_weight, with experts switchback_backward_weight_experts: dW[e]
  *   = dY^T X over the rows of expert e, 16-bit operands, binary32 accumulation; zeros for an expert without rows.  dw
  *   [experts,m,n], SB_BF16 or SB_F32; ws: switchback_backward_weight_experts_workspace_bytes(b, n, m, experts) bytes. */
@@ -268,6 +270,7 @@ int switchback_matmul_f8_block(const uint8_t *aq, sb_f8_format fmt_a, const uint
 int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint8_t *scales_w, const int32_t *offsets,
                                int64_t experts, int64_t b, int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, void *y,
                                sb_dtype y_dtype, void *ws, size_t ws_bytes, void *stream);
+size_t switchback_linear_f8_block_workspace_bytes(int64_t b, int64_t n, int64_t m, int64_t experts);
 int switchback_forward_f8_block(const void *x_bf16, const void *w_bf16, const int32_t *offsets, int64_t experts, int64_t b,
                                 int64_t n, int64_t m, sb_f8_format fmt_x, sb_f8_format fmt_w, uint8_t *wq, uint8_t *scales_w,
                                 uint8_t *wq_t, uint8_t *scales_wt, void *y, sb_dtype y_dtype, void *ws, size_t ws_bytes,

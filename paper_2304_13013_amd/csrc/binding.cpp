@@ -222,7 +222,8 @@ PyMethodDef bound_methods[] = {SB_METHOD("dev", &dev),
                                SB_ENTRY(layer_norm),
                                SB_ENTRY(layer_norm_backward),
                                SB_ENTRY(workspace_bytes),
-                               SB_ENTRY(backward_weight_experts_workspace_bytes)};
+                               SB_ENTRY(backward_weight_experts_workspace_bytes),
+                               SB_ENTRY(linear_f8_block_workspace_bytes)};
 constexpr size_t ENTRIES = sizeof(bound_methods) / sizeof(bound_methods[0]) - CHECKS;
 
 // bind(dev, out, saved_type, entry) -> {name: built-in function}: the general forms of the checks, the ctypes structure of

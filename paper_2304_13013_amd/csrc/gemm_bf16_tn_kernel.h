@@ -48,7 +48,8 @@ struct ExpertTokens {
     int first, end;  // of the split
 };
 __device__ __forceinline__ ExpertTokens expert_tokens(const GemmBf16ExpertArgs &p, int expert, int split, int stage) {
-    const int first = min(max(p.offsets[expert], 0), p.b), end = min(max(p.offsets[expert + 1], first), p.b);
+    const int first = min(max(uniform_load(p.offsets + expert), 0), p.b);
+    const int end = min(max(uniform_load(p.offsets + expert + 1), first), p.b);
     const int per = ((end - first + p.splits - 1) / p.splits + stage - 1) / stage * stage;
     ExpertTokens t;
     t.first = __builtin_amdgcn_readfirstlane(min(first + split * per, end));

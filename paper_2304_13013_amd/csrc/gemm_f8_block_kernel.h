@@ -30,14 +30,6 @@ struct GemmBlockArgs {
     int runs;               // direct kernel: workgroups that share the row blocks of an expert and a column block
 };
 
-// What all lanes read alike and no kernel writes while this one runs comes through the scalar cache: a vector load would have to
-// be waited for behind all requests before it.
-template <class T>
-__device__ __forceinline__ T uniform_load(const T *from) {
-    typedef const T __attribute__((address_space(4))) constant;
-    return *reinterpret_cast<constant *>(reinterpret_cast<uintptr_t>(from));
-}
-
 // Rows of an expert: [first, end).
 __device__ __forceinline__ void expert_rows(const GemmBlockArgs &p, int e, int *first, int *end) {
     *first = 0;

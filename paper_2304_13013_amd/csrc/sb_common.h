@@ -27,6 +27,14 @@ __device__ __forceinline__ void wait_vmcnt() {
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
+// What all lanes read alike and no kernel writes while this one runs comes through the scalar cache: a vector load would have to
+// be waited for behind all requests before it.
+template <class T>
+__device__ __forceinline__ T uniform_load(const T *from) {
+    typedef const T __attribute__((address_space(4))) constant;
+    return *reinterpret_cast<constant *>(reinterpret_cast<uintptr_t>(from));
+}
+
 __device__ __forceinline__ float bf16_bits_to_float(unsigned int bits16) { return __uint_as_float(bits16 << 16); }
 
 // Launchers (each validates nothing: the C-ABI layer has already checked shapes and pointers).

@@ -457,16 +457,22 @@ int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint
     const int st = block_shape_status(b, n, m, experts, offsets != nullptr);
     if (st != SB_OK) return st;
     if (b == 0) return SB_OK;
-    if (!ok_ptr(x_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w) || !ok_ptr(y) || !ok_ptr(ws) || !aligned4(offsets)) return SB_INVALID_ARG;
-    if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
+    if (!ok_ptr(x_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w) || !ok_ptr(y) || !aligned4(offsets)) return SB_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (sb::few_rows(b, m, n, experts))
         return from_hip(sb::launch_gemm_f8_block_few(x_bf16, n, fmt_x, wq, fmt_w, scales_w, offsets, experts, b, m, y, y_dtype, s));
+    if (!ok_ptr(ws)) return SB_INVALID_ARG;
+    if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
     uint8_t *xq = static_cast<uint8_t *>(ws), *scales_x = xq + row_codes_bytes(b, n);
     const hipError_t e = sb::launch_quantize_rows_block(x_bf16, b, n, fmt_x, xq, scales_x, s);
     if (e != hipSuccess) return SB_HIP_ERROR;
     return from_hip(sb::launch_gemm_f8_block(xq, fmt_x, scales_x, wq, fmt_w, scales_w, offsets, experts, b, m, whole_blocks(n), y,
                                              y_dtype, s));
+}
+
+size_t switchback_linear_f8_block_workspace_bytes(int64_t b, int64_t n, int64_t m, int64_t experts) {
+    if (block_shape_status(b, n, m, experts, true) != SB_OK || b == 0 || sb::few_rows(b, m, n, experts)) return 0;
+    return block_workspace_bytes(b, n);
 }
 
 int switchback_forward_f8_block(const void *x_bf16, const void *w_bf16, const int32_t *offsets, int64_t experts, int64_t b,
@@ -600,7 +606,7 @@ size_t switchback_workspace_bytes(int op, int64_t b, int64_t n, int64_t m) {
         case SB_OP_LAYER_NORM_BACKWARD:  // x is [b, n]
             if (b < 0 || n <= 0 || n > 65536) return 0;
             return sb::layer_norm_backward_workspace_bytes(b, n);
-        case SB_OP_LINEAR_F8_BLOCK:
+        case SB_OP_FORWARD_F8_BLOCK:
             if (b < 0 || n <= 0) return 0;
             return block_workspace_bytes(b, n);
         default: return 0;

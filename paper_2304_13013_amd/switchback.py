@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(_HERE, "libswitchback.so")
 SB_BF16, SB_F32, SB_I32_RAW = 0, 1, 2
 SB_OP_QUANTIZE_TENSORWISE, SB_OP_FORWARD, SB_OP_BACKWARD_INPUT, SB_OP_BACKWARD_WEIGHT, SB_OP_QUANTIZE_COLWISE = 0, 1, 2, 3, 4
 SB_OP_STABLE_ADAMW = 5
-SB_OP_LAYER_NORM_BACKWARD, SB_OP_LINEAR_F8_BLOCK = 6, 7
+SB_OP_LAYER_NORM_BACKWARD, SB_OP_FORWARD_F8_BLOCK = 6, 7
 SB_E4M3, SB_E5M2 = 0, 1
 
 _TORCH_DTYPE = {SB_BF16: torch.bfloat16, SB_F32: torch.float32, SB_I32_RAW: torch.int32}
@@ -88,8 +88,9 @@ def load_library():
     lib.switchback_linear_f8_block.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, ci, vp, sz, vp]
     lib.switchback_forward_f8_block.argtypes = [vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, ci, vp, sz, vp]
     lib.switchback_backward_weight_experts.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, ci, vp, sz, vp]
-    lib.switchback_backward_weight_experts_workspace_bytes.argtypes = [i64, i64, i64, i64]
-    lib.switchback_backward_weight_experts_workspace_bytes.restype = sz
+    for name in ("switchback_linear_f8_block_workspace_bytes", "switchback_backward_weight_experts_workspace_bytes"):
+        getattr(lib, name).argtypes = [i64, i64, i64, i64]
+        getattr(lib, name).restype = sz
     lib.switchback_layer_norm.argtypes = [vp, ci, vp, vp, cf, i64, i64, vp, vp, vp, vp]
     lib.switchback_layer_norm_backward.argtypes = [vp, vp, ci, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
     lib.switchback_ceiling_mfma.argtypes = [ci, vp, sz, vp, sz, ci, ci, ci, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -700,11 +701,14 @@ def linear_f8_block(x, wq, scales_w, offsets=None, fmt_x=SB_E4M3, fmt_w=SB_E4M3,
     if y_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("y must be bf16 or f32")
     y = _out(y, (b, m), y_dtype, x.device, "y")
-    ws = _workspace(SB_OP_LINEAR_F8_BLOCK, b, n, 0, x.device) if ws is None else ws
+    if ws is None:
+        need = lib.switchback_linear_f8_block_workspace_bytes(b, n, m, experts)  # none for few rows
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _on_current_device(x, wq, scales_w, offsets, y, ws)
     _check(lib.switchback_linear_f8_block(
         _dev(x, torch.bfloat16, 2), _dev(wq, torch.uint8), _check_weight_scales(scales_w, lead, m, k, x.device), where, experts,
-        b, n, m, fmt_x, fmt_w, _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(ws), ws.numel() * ws.element_size(), _stream()))
+        b, n, m, fmt_x, fmt_w, _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream()))
     return y
 
 
@@ -718,7 +722,8 @@ class BlockBuffers:
         e = lambda *shape: torch.empty(lead + shape, dtype=torch.uint8, device=device)
         self.wq, self.scales_w = e(m, kn), e(km // 128, kn // 128)
         self.wq_t, self.scales_wt = e(n, km), e(kn // 128, km // 128)
-        self.ws = torch.empty(max(workspace_bytes(SB_OP_LINEAR_F8_BLOCK, b, n, 0), workspace_bytes(SB_OP_LINEAR_F8_BLOCK, b, m, 0), 16),
+        self.ws = torch.empty(max(workspace_bytes(SB_OP_FORWARD_F8_BLOCK, b, n, 0), 16,
+                                  _entries().switchback_linear_f8_block_workspace_bytes(b, m, n, experts or 1)),
                               dtype=torch.uint8, device=device)
         self.ws_dw = (_workspace(SB_OP_BACKWARD_WEIGHT, b, n, m, device) if experts is None else
                       _experts_workspace(b, n, m, experts, device))

@@ -63,10 +63,13 @@ def test_block_calls_refuse(lib):
     def linear(x=FAKE, w=FAKE, sw=FAKE, offsets=NULL, experts=1, b=4, n=64, m=64, fx=0, fw=0, y=FAKE, dtype=0, ws=FAKE, size=1 << 30):
         return lib.switchback_linear_f8_block(x, w, sw, offsets, experts, b, n, m, fx, fw, y, dtype, ws, size, NULL)
     assert linear(fx=2) == linear(fw=2) == linear(dtype=2) == linear(b=-1) == linear(experts=3) == INVALID
-    for name in ("x", "w", "sw", "y", "ws"):
+    for name in ("x", "w", "sw", "y"):
         assert linear(**{name: NULL}) == linear(**{name: ODD}) == INVALID, name
     assert linear(n=96) == linear(m=32) == SHAPE
-    assert linear(size=sb.workspace_bytes(sb.SB_OP_LINEAR_F8_BLOCK, 4, 64, 0) - 1) == WS
+    need = lib.switchback_linear_f8_block_workspace_bytes(4000, 1024, 1024, 1)
+    assert need == sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 4000, 1024, 0) and lib.switchback_linear_f8_block_workspace_bytes(4, 64, 64, 1) == 0
+    assert linear(b=4000, n=1024, m=1024, size=need - 1) == WS and linear(b=4000, n=1024, m=1024, ws=NULL) == INVALID
+    assert linear(b=4000, n=1024, m=1024, ws=ODD) == INVALID
     assert linear(b=0, x=NULL, y=NULL, ws=NULL, size=0) == 0
 
     def forward(x=FAKE, w=FAKE, offsets=NULL, experts=1, b=4, n=64, m=64, fx=0, fw=0, wq=FAKE, sw=FAKE, wt=FAKE, st=FAKE, y=FAKE, dtype=0,
@@ -142,9 +145,11 @@ def test_tensors_of_another_gpu_are_refused(monkeypatch):
 
 
 def test_workspaces(lib):
-    assert sb.workspace_bytes(sb.SB_OP_LINEAR_F8_BLOCK, 100, 64, 0) == 100 * 128 + 100 * 4       # codes of whole blocks, a dword of scales a row
-    assert sb.workspace_bytes(sb.SB_OP_LINEAR_F8_BLOCK, 3, 1088, 0) == -(-3 * 1152 // 256) * 256 + 3 * 12
+    assert sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 100, 64, 0) == 100 * 128 + 100 * 4       # codes of whole blocks, a dword of scales a row
+    assert sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 3, 1088, 0) == -(-3 * 1152 // 256) * 256 + 3 * 12
     bufs = sb.BlockBuffers(7, 192, 320, 3, "cpu")
     assert tuple(bufs.wq.shape) == (3, 320, 256) and tuple(bufs.wq_t.shape) == (3, 192, 384)
     assert tuple(bufs.scales_w.shape) == (3, 3, 2) and tuple(bufs.scales_wt.shape) == (3, 2, 3)
-    assert bufs.ws.numel() >= max(sb.workspace_bytes(sb.SB_OP_LINEAR_F8_BLOCK, 7, k, 0) for k in (192, 320))
+    assert bufs.ws.numel() >= sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 7, 192, 0)
+    big = sb.BlockBuffers(4000, 192, 2048, None, "cpu")
+    assert big.ws.numel() >= sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 4000, 2048, 0) == lib.switchback_linear_f8_block_workspace_bytes(4000, 2048, 192, 1)

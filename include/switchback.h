@@ -239,9 +239,10 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  * numbers: rows offsets[e] .. offsets[e+1] - 1 of X, Y, dX and dY are expert e's (none if the two are equal).  Rows before
  * offsets[0] and from offsets[experts] on belong to no expert: their outputs are left as they were.  Offsets are read when the
  * call's kernels run, not on the host, and clamped to 0 .. b: others than documented give unspecified values, never a fault.
- * 1 <= experts <= 1024.
+ * 1 <= experts <= 1024.  Outputs and workspaces overlap neither each other nor the inputs.
  *
- * switchback_quantize_rowwise_f8_block: x [rows,cols] bf16 -> codes [rows,K], scales [S,rows,4].  cols % 8 == 0, cols <= 131072.
+ * switchback_quantize_rowwise_f8_block: x [rows,cols] bf16 -> codes [rows,K], scales [S,rows,4].  cols % 8 == 0, cols <= 131072,
+ *   rows * ceil(cols / 512) <= 2^27.
  * switchback_quantize_weight_f8_block: w [experts,m,n] bf16 -> codes [experts,m,K(n)], scales [experts,ceil(m/128),K(n)/128]
  *   and, unless NULL, the transpose: codes_t [experts,n,K(m)], scales_t [experts,ceil(n/128),K(m)/128].  m % 64 == 0,
  *   n % 64 == 0.
@@ -288,7 +289,8 @@ size_t switchback_backward_weight_experts_workspace_bytes(int64_t b, int64_t n, 
  *   dy, dx [rows,cols] in dtype; mean, rstd as the forward pass left them; gamma [cols] f32 or NULL; dgamma, dbeta [cols] f32,
  *   either or both NULL; their sums are formed in a fixed order (deterministic; no rows give zeros).
  *   ws: SB_OP_LAYER_NORM_BACKWARD workspace (0 bytes for few rows; not needed if dgamma and dbeta are NULL).
- * 1 <= cols <= 65536, rows <= 2^30; matrices, gamma and beta 16-byte aligned (dgamma, dbeta, mean, rstd 4-byte). */
+ * 1 <= cols <= 65536, rows <= 2^30; matrices, gamma and beta 16-byte aligned (dgamma, dbeta, mean, rstd 4-byte).  Outputs and
+ * the workspace overlap neither each other nor the inputs: y = x and dx = dy are refused. */
 int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, const float *beta, float eps, int64_t rows,
                           int64_t cols, void *y, float *mean, float *rstd, void *stream);
 int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype, const float *mean, const float *rstd,

@@ -190,8 +190,8 @@ inline ProductPlan plan_product(int64_t M, int64_t N, int64_t K, ProductKind kin
 // Whether rows in 16 bit go to the kernel that quantizes them itself, 16 at a time, and reads a weight once for each 16 rows: 16
 // rows, or four an expert in the mean; and small products, where the launch of the quantizer would be most of the time.  Two
 // launches / this one (us): 16 rows, 4096 -> 16384 from memory 17.6 / 15.5; 64 rows, 1024 -> 1024 6.3 / 4.0; 512 rows, 1024 ->
-// 256 7.0 / 4.1; 1024 rows, 512 -> 512 7.1 / 5.8; 32 rows, 4096 -> 4096 8.1 / 7.6; 256 rows, 32 experts of 1024 x 1024 11.5 / 8.8; on the
-// other side 64 rows, 4096 -> 4096 9.1 / 11.6; 128 rows, 8192 -> 512 11.5 / 12.1.
+// 256 7.0 / 4.1; 1024 rows, 512 -> 512 7.1 / 5.8; 32 rows, 4096 -> 4096 8.1 / 7.6; 256 rows, 32 experts of 1024 x 1024 11.5 /
+// 8.8; on the other side 64 rows, 4096 -> 4096 9.1 / 11.6; 128 rows, 8192 -> 512 11.5 / 12.1.
 inline bool plan_few_rows(int64_t M, int64_t N, int64_t K, int64_t experts) {
     if (M <= 16 || (M <= 4 * experts && M <= 1024)) return true;
     const int64_t used = experts < M ? experts : M, even = experts == 1 ? (M + 15) / 16 : (M + 8 * used + 15) / 16;
@@ -209,9 +209,10 @@ inline int plan_few_runs(int64_t M, int64_t experts) {
 // take a row block cut short per expert, or one block each where there are fewer rows than that.
 //
 // The estimates are those of the plain products, and the weights' way from memory at 5.2 TB/s, which the small-product kernel
-// reaches (256 rows, 8 experts of 4096 x 4096: 25.5 us, 40.5 on tiles) and which the tiles hide in part (1000 rows, 64 experts
-// of 2048 x 2048: 41.8 / 70.4; 30000 rows, 64 experts of 2048 x 1024: 82 on tiles, 75 by the plain estimate).  Twice the row blocks of an even share: experts with more rows than others find workgroups for them (2000 rows,
-// 16 experts of 4096 x 1024: 30.6 / 29.6 us; 1000 rows, 8 of 2048 x 2048: 18.4 / 16.9).
+// reaches (256 rows, 8 experts of 4096 x 4096: 25.5 us, 40.5 on tiles) and which the tiles hide in part (1000 rows, 64 experts of
+// 2048 x 2048: 41.8 / 70.4; 30000 rows, 64 experts of 2048 x 1024: 82 on tiles, 75 by the plain estimate).  Twice the row blocks
+// of an even share: experts with more rows than others find workgroups for them (2000 rows, 16 experts of 4096 x 1024: 30.6 /
+// 29.6 us; 1000 rows, 8 of 2048 x 2048: 18.4 / 16.9).
 struct ExpertProductPlan {
     TileKind rest;
     int split, runs;

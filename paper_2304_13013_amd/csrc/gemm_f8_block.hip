@@ -34,14 +34,14 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
 #define WAVES_W256 __attribute__((amdgpu_waves_per_eu(1, 1)))  // one wave per SIMD: all 512 registers are a lane's
 #define WAVES_W128 __attribute__((amdgpu_waves_per_eu(1, 1)))
 // name suffix: format of the token-side operand, then of the weight-side operand (4 = E4M3, 5 = E5M2)
-#define SB_BLOCK_ENTRIES(ENTRY, name, CFG)                        \
-    ENTRY(name##_a4b4_bf16, CFG, OUT_BF16, 0, 0)  \
-    ENTRY(name##_a4b4_f32, CFG, OUT_F32, 0, 0)    \
-    ENTRY(name##_a5b4_bf16, CFG, OUT_BF16, 1, 0)  \
-    ENTRY(name##_a5b4_f32, CFG, OUT_F32, 1, 0)    \
-    ENTRY(name##_a4b5_bf16, CFG, OUT_BF16, 0, 1)  \
-    ENTRY(name##_a4b5_f32, CFG, OUT_F32, 0, 1)    \
-    ENTRY(name##_a5b5_bf16, CFG, OUT_BF16, 1, 1)  \
+#define SB_BLOCK_ENTRIES(ENTRY, name, CFG)       \
+    ENTRY(name##_a4b4_bf16, CFG, OUT_BF16, 0, 0) \
+    ENTRY(name##_a4b4_f32, CFG, OUT_F32, 0, 0)   \
+    ENTRY(name##_a5b4_bf16, CFG, OUT_BF16, 1, 0) \
+    ENTRY(name##_a5b4_f32, CFG, OUT_F32, 1, 0)   \
+    ENTRY(name##_a4b5_bf16, CFG, OUT_BF16, 0, 1) \
+    ENTRY(name##_a4b5_f32, CFG, OUT_F32, 0, 1)   \
+    ENTRY(name##_a5b5_bf16, CFG, OUT_BF16, 1, 1) \
     ENTRY(name##_a5b5_f32, CFG, OUT_F32, 1, 1)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d32, D32)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d64, D64)

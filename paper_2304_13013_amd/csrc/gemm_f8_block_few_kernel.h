@@ -1,14 +1,15 @@
 // The block-scaled float8 layer for a few rows (a token each of a few sequences), plain and by experts: rows in 16 bit, weights
 // in codes, hand-written for gfx950.  gemm_f8_block_kernel.h has the definition.
 //
-// What bounds it: the weights' way from memory, and the launches.  So the rows are not quantized by a launch of their own (3
-// us of 15 for 16 rows through 4096 -> 16384): every wave fetches its blocks of k of the rows as they are and makes their
-// codes and scales in registers, in the shadow of the requests in flight.  A workgroup owns 32 columns of one weight, its four
-// waves split the contraction, each with an LDS ring of two stages of 128 k (4 KiB of weights, 4 KiB of rows) that it alone
-// fills and reads; two workgroups share a compute unit, so that 64 KiB of weights are on their way to each.  Weights are requested as non-temporal: nobody reads them again (4 rows, 4096 -> 16384 from memory: 15.4 ->
-// 13.7 us, 4.9 TB/s).  Slower: 64 columns a workgroup, one on a compute unit (32 experts of 1024 x 4096, 48 rows: 31 -> 36 us;
-// 16 rows, 4096 -> 16384: 16.9 -> 15.6); rows straight into registers, four stages ahead (16.7 for 14.1 us);
-// eight waves where there is a workgroup a compute unit (8 rows, 8192 -> 8192: 13.6 -> 16.5; 16 rows, 16384 -> 4096: 23.7 -> 22.1).
+// What bounds it: the weights' way from memory, and the launches.  So the rows are not quantized by a launch of their own (3 us
+// of 15 for 16 rows through 4096 -> 16384): every wave fetches its blocks of k of the rows as they are and makes their codes and
+// scales in registers, in the shadow of the requests in flight.  A workgroup owns 32 columns of one weight, its four waves split
+// the contraction, each with an LDS ring of two stages of 128 k (4 KiB of weights, 4 KiB of rows) that it alone fills and reads;
+// two workgroups share a compute unit, so that 64 KiB of weights are on their way to each.  Weights are requested as
+// non-temporal: nobody reads them again (4 rows, 4096 -> 16384 from memory: 15.4 -> 13.7 us, 4.9 TB/s).  Not kept: 64 columns a
+// workgroup, one on a compute unit (32 experts of 1024 x 4096, 48 rows: 31 -> 36 us, though 16 rows, 4096 -> 16384, without
+// non-temporal requests, 16.9 -> 15.6); rows straight into registers, four stages ahead (14.1 -> 16.7 us); eight waves where there
+// is a workgroup a compute unit (8 rows, 8192 -> 8192: 13.6 -> 16.5, though 16 rows, 16384 -> 4096: 23.7 -> 22.1).
 // v_mfma_scale_f32_16x16x128_f8f6f4 takes a block of k at once: 16 rows, the weight's columns as the first operand, so that a
 // lane owns one row and four columns.  Rows past the last one are not fetched.  More than 16 rows of a weight are worked off 16 at
 // a time, by `runs` workgroups, the weight read again by each: the dispatch sees to it that they are rare, or the product

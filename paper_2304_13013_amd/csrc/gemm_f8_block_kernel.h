@@ -67,8 +67,6 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
     const int n0 = block * C::COLS;
     int first, end;
     expert_rows(p, expert, &first, &end);
-    first = __builtin_amdgcn_readfirstlane(first);
-    end = __builtin_amdgcn_readfirstlane(end);
     const int KB = p.K / C::BK;
     const int s0 = (int)((long long)wave * KB / C::WAVES), s1 = (int)((long long)(wave + 1) * KB / C::WAVES), n = s1 - s0;
 

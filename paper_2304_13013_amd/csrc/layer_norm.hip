@@ -3,11 +3,11 @@
 //   mu = mean_j x,  r = 1 / sqrt(mean_j (x - mu)^2 + eps),  h = (x - mu) r,  y = h gamma + beta
 //   a = dy gamma,   dx = r (a - mean_j a - h mean_j(a h)),  dgamma_j = sum_i dy h,  dbeta_j = sum_i dy
 //
-// What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences
-// from it (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large).  Rows of up to 2048 columns
-// belong to a wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and beta (or its
-// shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read from
-// L2 again.  Arithmetic is binary32; y and dx are rounded once.
+// What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences from it
+// (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large).  Rows of up to 2048 columns belong to a
+// wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and
+// beta (or its shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read
+// from L2 again.  Arithmetic is binary32; y and dx are rounded once.
 //
 // The sums over the rows: every workgroup adds its rows' terms in registers, its waves' sums meet in LDS and go to the
 // workspace, and a second launch adds those in a fixed order.  No atomics: the same inputs give the same bits.
@@ -259,10 +259,9 @@ __device__ __forceinline__ void column_sums(const T *__restrict__ dy, const T *_
 }
 
 // SUMS: the rows' terms of dgamma and dbeta are added up and left in partial[blockIdx.x][2][cols].  Without, workgroups from
-// row_blocks on form the sums of 16 columns each from the rows themselves: for few rows, which lie in L2 and are read twice sooner
-// than a second launch starts.  gamma lies in LDS, four
-// consecutive elements of a lane at a time and lanes side by side: in registers, next to the sums and two rows, it would
-// leave one wave per SIMD.
+// row_blocks on form the sums of 16 columns each from the rows themselves: for few rows, which lie in L2 and are read twice
+// sooner than a second launch starts.  gamma lies in LDS, four consecutive elements of a lane at a time and lanes side by side:
+// in registers, next to the sums and two rows, it would leave one wave per SIMD.
 template <class T, int V, int P, int LANES, bool SUMS>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean, const float *__restrict__ rstd,

@@ -54,6 +54,13 @@ int weight_gradient_workspace_status(const sb::WeightGradPlan &plan, int64_t n, 
     return ws_bytes < need ? SB_WORKSPACE_TOO_SMALL : SB_OK;
 }
 
+// Whether `rows` rows of `row_a` and `row_b` bytes have memory in common.
+bool overlap(const void *a, int64_t row_a, const void *b, int64_t row_b, int64_t rows) {
+    const uintptr_t from_a = reinterpret_cast<uintptr_t>(a), from_b = reinterpret_cast<uintptr_t>(b);
+    return from_a < from_b + (uint64_t)(rows * row_b) && from_b < from_a + (uint64_t)(rows * row_a);
+}
+int bytes_of(sb_dtype t) { return t == SB_BF16 ? 2 : 4; }
+
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 int64_t whole_blocks(int64_t cols) { return (cols + 127) / 128 * 128; }
 
@@ -417,7 +424,7 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
 int switchback_quantize_rowwise_f8_block(const void *x_bf16, int64_t rows, int64_t cols, sb_f8_format fmt, uint8_t *codes,
                                          uint8_t *scales, void *stream) {
     if (rows < 0 || cols <= 0 || !ok_f8(fmt)) return SB_INVALID_ARG;
-    if (cols % 8 || cols > kMaxIntK || rows > (int64_t)1 << 30 || rows * ((cols + 511) / 512) > (int64_t)1 << 32)
+    if (cols % 8 || cols > kMaxIntK || rows > (int64_t)1 << 30 || rows * ((cols + 511) / 512) > (int64_t)1 << 27)
         return SB_UNSUPPORTED_SHAPE;
     if (rows == 0) return SB_OK;
     if (!ok_ptr(x_bf16) || !ok_ptr(codes) || !ok_ptr(scales)) return SB_INVALID_ARG;
@@ -459,10 +466,12 @@ int switchback_linear_f8_block(const void *x_bf16, const uint8_t *wq, const uint
     if (b == 0) return SB_OK;
     if (!ok_ptr(x_bf16) || !ok_ptr(wq) || !ok_ptr(scales_w) || !ok_ptr(y) || !aligned4(offsets)) return SB_INVALID_ARG;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (sb::few_rows(b, m, n, experts))
+    const bool few = sb::few_rows(b, m, n, experts);
+    if (!few && !ok_ptr(ws)) return SB_INVALID_ARG;
+    if (!few && ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
+    if (overlap(x_bf16, 2 * n, y, bytes_of(y_dtype) * m, b)) return SB_INVALID_ARG;
+    if (few)
         return from_hip(sb::launch_gemm_f8_block_few(x_bf16, n, fmt_x, wq, fmt_w, scales_w, offsets, experts, b, m, y, y_dtype, s));
-    if (!ok_ptr(ws)) return SB_INVALID_ARG;
-    if (ws_bytes < block_workspace_bytes(b, n)) return SB_WORKSPACE_TOO_SMALL;
     uint8_t *xq = static_cast<uint8_t *>(ws), *scales_x = xq + row_codes_bytes(b, n);
     const hipError_t e = sb::launch_quantize_rows_block(x_bf16, b, n, fmt_x, xq, scales_x, s);
     if (e != hipSuccess) return SB_HIP_ERROR;
@@ -524,6 +533,7 @@ int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, con
     if (cols > 65536 || rows > (int64_t)1 << 30) return SB_UNSUPPORTED_SHAPE;
     if (rows == 0) return SB_OK;
     if (!ok_ptr(x) || !ok_ptr(y) || !aligned16(gamma) || !aligned16(beta) || !aligned4(mean) || !aligned4(rstd)) return SB_INVALID_ARG;
+    if (overlap(x, cols * bytes_of(dtype), y, cols * bytes_of(dtype), rows)) return SB_INVALID_ARG;
     return from_hip(sb::launch_layer_norm(x, gamma, beta, eps, rows, cols, dtype == SB_BF16, y, mean, rstd,
                                           static_cast<hipStream_t>(stream)));
 }
@@ -539,6 +549,8 @@ int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype
     const size_t need = sums ? sb::layer_norm_backward_workspace_bytes(rows, cols) : 0;
     if (need > 0 && !ok_ptr(ws)) return SB_INVALID_ARG;
     if (ws_bytes < need) return SB_WORKSPACE_TOO_SMALL;
+    const int64_t row = cols * bytes_of(dtype);
+    if (overlap(dx, row, x, row, rows) || overlap(dx, row, dy, row, rows)) return SB_INVALID_ARG;
     return from_hip(sb::launch_layer_norm_backward(dy, x, mean, rstd, gamma, rows, cols, dtype == SB_BF16, dx, dgamma, dbeta, ws,
                                                    static_cast<hipStream_t>(stream)));
 }

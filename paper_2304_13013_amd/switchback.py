@@ -208,7 +208,8 @@ def _device_of_general(*tensors):
     return -1 if not at else at.pop() if len(at) == 1 else -2
 
 
-_dev, _out, _device_of = _dev_general, _out_general, _device_of_general  # until _bind() puts the built-in forms here, which hand on what is not plain
+# until _bind() puts the built-in forms here, which hand on what is not plain
+_dev, _out, _device_of = _dev_general, _out_general, _device_of_general
 
 
 def _check_bufs(bufs, b, n, m):
@@ -601,6 +602,11 @@ def _on_current_device(*tensors):
                               % ("several GPUs" if at < 0 else "GPU %d" % at, _current_device()))
 
 
+def _given_ws(ws):
+    """Address and bytes of a workspace, or of none."""
+    return (None, 0) if ws is None else (_dev(ws, ws.dtype), ws.numel() * ws.element_size())
+
+
 def _whole_blocks(cols):
     return -(-cols // 128) * 128
 
@@ -705,16 +711,17 @@ def linear_f8_block(x, wq, scales_w, offsets=None, fmt_x=SB_E4M3, fmt_w=SB_E4M3,
         need = lib.switchback_linear_f8_block_workspace_bytes(b, n, m, experts)  # none for few rows
         ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _on_current_device(x, wq, scales_w, offsets, y, ws)
+    ws_at, ws_bytes = _given_ws(ws)
     _check(lib.switchback_linear_f8_block(
         _dev(x, torch.bfloat16, 2), _dev(wq, torch.uint8), _check_weight_scales(scales_w, lead, m, k, x.device), where, experts,
-        b, n, m, fmt_x, fmt_w, _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(ws),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+        b, n, m, fmt_x, fmt_w, _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], ws_at, ws_bytes, _stream()))
     return y
 
 
 class BlockBuffers:
     """Device buffers of one block-scaled float8 layer of shape (b, n, m), or of `experts` such layers that share b rows,
-    allocated once: the weight's codes and scales in both layouts, and the workspaces."""
+    allocated once: the weight's codes and scales in both layouts, and the workspaces, which one call at a time uses (those of
+    one stream follow each other)."""
 
     def __init__(self, b, n, m, experts=None, device="cuda"):
         self.b, self.n, self.m, self.experts = b, n, m, experts
@@ -752,9 +759,9 @@ def forward_f8_block(x, w, bufs=None, offsets=None, y=None, y_dtype=torch.bfloat
     y = _out(y, (b, m), y_dtype, x.device, "y")
     _on_current_device(x, w, offsets, y, bufs.wq)
     _check(lib.switchback_forward_f8_block(
-        _dev(x, torch.bfloat16, 2), _dev(w, torch.bfloat16), where, experts, b, n, m, fmt_x, fmt_w, _ptr(bufs.wq),
-        _ptr(bufs.scales_w), _ptr(bufs.wq_t), _ptr(bufs.scales_wt), _dev(y, y_dtype, 2), _SB_DTYPE[y_dtype], _ptr(bufs.ws),
-        bufs.ws.numel(), _stream()))
+        _dev(x, torch.bfloat16, 2), _dev(w, torch.bfloat16), where, experts, b, n, m, fmt_x, fmt_w, _dev(bufs.wq, torch.uint8),
+        _dev(bufs.scales_w, torch.uint8), _dev(bufs.wq_t, torch.uint8), _dev(bufs.scales_wt, torch.uint8), _dev(y, y_dtype, 2),
+        _SB_DTYPE[y_dtype], _dev(bufs.ws, torch.uint8), bufs.ws.numel(), _stream()))
     return y, bufs
 
 
@@ -771,8 +778,8 @@ def backward_input_f8_block(dy, bufs, offsets=None, dx=None, dx_dtype=torch.bflo
     dx = _out(dx, (b, bufs.n), dx_dtype, dy.device, "dx")
     _on_current_device(dy, offsets, dx, bufs.wq)
     _check(lib.switchback_linear_f8_block(
-        _dev(dy, torch.bfloat16, 2), _ptr(bufs.wq_t), _ptr(bufs.scales_wt), where, bufs.experts or 1, b, m, bufs.n, fmt_g, fmt_w,
-        _dev(dx, dx_dtype, 2), _SB_DTYPE[dx_dtype], _ptr(bufs.ws), bufs.ws.numel(), _stream()))
+        _dev(dy, torch.bfloat16, 2), _dev(bufs.wq_t, torch.uint8), _dev(bufs.scales_wt, torch.uint8), where, bufs.experts or 1, b, m,
+        bufs.n, fmt_g, fmt_w, _dev(dx, dx_dtype, 2), _SB_DTYPE[dx_dtype], _dev(bufs.ws, torch.uint8), bufs.ws.numel(), _stream()))
     return dx
 
 
@@ -790,6 +797,8 @@ def backward_weight_experts(dy, x, offsets, bufs=None, dw=None, dw_dtype=torch.b
         raise SwitchBackError("dy [b,m] and x [b,n] disagree on b")
     where = _dev(offsets, torch.int32, 1)
     experts = offsets.numel() - 1
+    if experts < 1:
+        raise SwitchBackError("offsets must hold an entry more than there are experts")
     if bufs is not None:
         _check_block_bufs(bufs, b, n, m, (experts,))
     ws = bufs.ws_dw if bufs is not None else _experts_workspace(b, n, m, experts, dy.device)
@@ -799,7 +808,7 @@ def backward_weight_experts(dy, x, offsets, bufs=None, dw=None, dw_dtype=torch.b
     dw = _out(dw, (experts, m, n), dw_dtype, dy.device, "dw")
     _on_current_device(dy, x, offsets, dw, ws)
     _check(lib.switchback_backward_weight_experts(_dev(dy, torch.bfloat16, 2), _dev(x, torch.bfloat16, 2), where, experts, b, n, m,
-                                                  _dev(dw, dw_dtype, 3), _SB_DTYPE[dw_dtype], _ptr(ws), ws.numel(), _stream()))
+                                                  _dev(dw, dw_dtype, 3), _SB_DTYPE[dw_dtype], _dev(ws, torch.uint8), ws.numel(), _stream()))
     return dw
 
 
@@ -845,10 +854,11 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, affine=True, dx=None, dga
     elif dgamma is not None or dbeta is not None:
         raise SwitchBackError("affine=False computes neither dgamma nor dbeta")
     _on_current_device(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, ws)
+    ws_at, ws_bytes = _given_ws(ws)
     _check(lib.switchback_layer_norm_backward(
         _dev(dy, dtype, 2), _dev(x, dtype, 2), _SB_DTYPE[dtype], _dev(mean, torch.float32), _dev(rstd, torch.float32),
         _vec(gamma, cols, x.device, "gamma"), rows, cols, _dev(dx, dtype, 2), _dev(dgamma, torch.float32, 1) if affine else None,
-        _dev(dbeta, torch.float32, 1) if affine else None, _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+        _dev(dbeta, torch.float32, 1) if affine else None, ws_at, ws_bytes, _stream()))
     return dx, dgamma, dbeta
 
 

@@ -394,3 +394,28 @@ def test_captured_in_graphs_and_on_two_streams():
             t["step"]()
             torch.cuda.synchronize()
             assert all(torch.equal(v, t["keep"][name]) for name, v in replayed.items()), "replay %d" % i
+
+
+def test_memory_that_no_kernel_may_touch_is_refused():
+    """Workspaces and buffers on the host, outputs over inputs."""
+    x, dy, w = (torch.randn(600, 1024, device=DEV).bfloat16(), torch.randn(600, 1024, device=DEV).bfloat16(), torch.randn(1024, 1024, device=DEV).bfloat16())
+    y, bufs = sb.forward_f8_block(x, w)
+    need = sb.load_library().switchback_linear_f8_block_workspace_bytes(600, 1024, 1024, 1)
+    assert need > 0
+    with pytest.raises(sb.SwitchBackError):
+        sb.linear_f8_block(x, bufs.wq, bufs.scales_w, ws=torch.zeros(need, dtype=torch.uint8))
+    with pytest.raises(sb.SwitchBackError):
+        sb.forward_f8_block(x, w, sb.BlockBuffers(600, 1024, 1024, None, "cpu"))
+    with pytest.raises(sb.SwitchBackError):
+        sb.backward_input_f8_block(dy, sb.BlockBuffers(600, 1024, 1024, None, "cpu"))
+    with pytest.raises(sb.SwitchBackError):
+        sb.backward_weight_experts(dy, x, torch.tensor([0, 600], dtype=torch.int32, device=DEV), sb.BlockBuffers(600, 1024, 1024, 1, "cpu"))
+    for rows in (600, 4):
+        with pytest.raises(sb.SwitchBackError):
+            sb.backward_input_f8_block(dy[:rows], sb.BlockBuffers(rows, 1024, 1024), dx=dy[:rows])
+        with pytest.raises(sb.SwitchBackError):
+            sb.linear_f8_block(x[:rows], bufs.wq, bufs.scales_w, y=x[:rows])
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    assert torch.equal(sb.linear_f8_block(x, bufs.wq, bufs.scales_w, ws=ws), y)
+    with pytest.raises(sb.SwitchBackError):
+        sb.layer_norm(x, y=x)

@@ -153,3 +153,33 @@ def test_workspaces(lib):
     assert bufs.ws.numel() >= sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 7, 192, 0)
     big = sb.BlockBuffers(4000, 192, 2048, None, "cpu")
     assert big.ws.numel() >= sb.workspace_bytes(sb.SB_OP_FORWARD_F8_BLOCK, 4000, 2048, 0) == lib.switchback_linear_f8_block_workspace_bytes(4000, 2048, 192, 1)
+
+
+def test_memory_in_common_is_refused(lib):
+    """A row that is written while others are still read: the calls that allow no output over an input say so."""
+    at = lambda i: ctypes.c_void_p(0x100000 + i)  # never dereferenced
+    far = at(1 << 20)
+    norm = lambda x, y: lib.switchback_layer_norm(x, 0, NULL, NULL, 1e-5, 4, 64, y, NULL, NULL, NULL)
+    back = lambda dy, x, dx: lib.switchback_layer_norm_backward(dy, x, 1, FAKE, FAKE, NULL, 4, 64, dx, NULL, NULL, NULL, 0, NULL)
+    assert norm(at(0), at(0)) == norm(at(0), at(4 * 64 * 2 - 16)) == norm(at(16), at(0)) == INVALID
+    assert back(at(0), far, at(0)) == back(far, at(0), at(4 * 64 * 4 - 16)) == back(at(16), far, at(0)) == INVALID
+
+    def linear(x, y, dtype, b=4, m=128):
+        return lib.switchback_linear_f8_block(x, FAKE, FAKE, NULL, 1, b, 64, m, 0, 0, y, dtype, far, 1 << 30, NULL)
+    assert linear(at(0), at(0), 0) == linear(at(0), at(4 * 64 * 2 - 16), 0) == linear(at(4 * 128 * 4 - 16), at(0), 1) == INVALID
+    assert linear(at(0), at(0), 0, 4000, 2048) == INVALID
+
+
+def test_workspaces_of_the_callers_lie_on_the_gpu():
+    for ws in (torch.zeros(64, dtype=torch.uint8), torch.zeros(64)):
+        with pytest.raises(sb.SwitchBackError):
+            sb._given_ws(ws)
+    assert sb._given_ws(None) == (None, 0)
+    with pytest.raises(sb.SwitchBackError):
+        sb.backward_weight_experts(torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(0, dtype=torch.int32))
+
+
+def test_most_rows_of_a_launch(lib):
+    """A workgroup for 16 rows of 512 columns: a launch has fewer than 2^32 threads."""
+    rows = lambda rows, cols: lib.switchback_quantize_rowwise_f8_block(FAKE, rows, cols, 0, FAKE, FAKE, NULL)
+    assert rows((1 << 27) + 1, 8) == rows(1 << 26, 1032) == rows(1 << 20, 131072) == SHAPE

@@ -244,7 +244,8 @@ def test_serving_a_few_rows(b, n, m, experts, rest, fmt):
 
 
 @pytest.mark.parametrize("b,n,m,experts", [(1, 64, 64, 1), (3, 64, 128, 3), (1000, 128, 64, 2), (5000, 320, 192, 3), (3001, 1088, 576, 9),
-                                           (777, 256, 320, 40), (20000, 256, 256, 2), (4100, 1280, 768, 5), (0, 64, 192, 4), (12000, 64, 1216, 6)])
+                                           (777, 256, 320, 40), (20000, 256, 256, 2), (4100, 1280, 768, 5), (0, 64, 192, 4), (12000, 64, 1216, 6),
+                                           (300, 1088, 1216, 24), (2500, 1344, 1344, 12), (40, 704, 960, 64)])
 def test_weight_gradient_of_experts(b, n, m, experts):
     """Small tiles and large ones, split sums and whole ones, experts without rows, rows of no expert (which may hold NaN)."""
     gen = torch.Generator().manual_seed(b + n)

@@ -15,7 +15,7 @@
 // This kernel: a workgroup owns 64 or 32 columns of one b and works through blocks of as many rows, its waves split the
 // contraction, each with an LDS ring of its own, and the partial sums meet in LDS (as in gemm_i8_direct_kernel.h, whose
 // operand path it shares: swizzled requests of 128-byte row segments straight into LDS).  Few rows are bound by the weights'
-// way from memory.
+// way from memory: 256 rows, 8 experts of 4096 x 4096 25.5 us, 5.3 TB/s of weights.
 #pragma once
 #include "gemm_i8_direct_kernel.h"
 

@@ -14,6 +14,9 @@
 //     its share of the experts (offsets are read once, when the kernel starts), so that the expert of a tile row is a ballot.
 //     A tile's rows start where its expert's do: the last one of an expert is cut short by the output's bounds check.
 //   * The epilogue has nothing to scale.
+// 16384 x 16384, K = 4096: 757-790 us, 2.8-2.9 PFLOP/s; 32896 x 1280, K = 5120: 183-190 us; 4 % above the product with one state
+// per row, for the scales' requests and reads.  What bounds it is what bounds that one: the clock under the instructions' power,
+// the operands' way into LDS, the tile boundary at short K.
 #pragma once
 #include "gemm_f8_block_kernel.h"
 #include "gemm_i8_wide_kernel.h"

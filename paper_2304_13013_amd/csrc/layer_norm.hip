@@ -8,6 +8,8 @@
 // wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and
 // beta (or its shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read
 // from L2 again.  Arithmetic is binary32; y and dx are rounded once.
+// 32896 x 1280 bf16: forward 29 us, 5.8 TB/s; backward 46 us and 4.5 for the sums' reduction, 5.0 TB/s; f32 11237 x 1088 backward
+// 28.5 + 4.
 //
 // The sums over the rows: every workgroup adds its rows' terms in registers, its waves' sums meet in LDS and go to the
 // workspace, and a second launch adds those in a fixed order.  No atomics: the same inputs give the same bits.

@@ -420,3 +420,51 @@ def test_memory_that_no_kernel_may_touch_is_refused():
     assert torch.equal(sb.linear_f8_block(x, bufs.wq, bufs.scales_w, ws=ws), y)
     with pytest.raises(sb.SwitchBackError):
         sb.layer_norm(x, y=x)
+
+
+def test_serving_captured_in_a_graph():
+    """The few-rows kernel, replayed with other rows and offsets."""
+    b, n, m, experts = 13, 320, 192, 5
+    gen = torch.Generator().manual_seed(4)
+    w = torch.randn(experts, m, n, generator=gen).bfloat16().to(DEV)
+    codes, scales, _, _ = sb.quantize_weight_f8_block(w, E4M3)
+    x, y = torch.zeros(b, n, dtype=torch.bfloat16, device=DEV), torch.zeros(b, m, dtype=torch.bfloat16, device=DEV)
+    where = torch.zeros(experts + 1, dtype=torch.int32, device=DEV)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        sb.linear_f8_block(x, codes, scales, offsets=where, y=y)
+    for i in range(4):
+        x.copy_(torch.randn(b, n, generator=gen).bfloat16())
+        where.copy_(torch.tensor(random_offsets(b, experts, gen, 0, i), dtype=torch.int32))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = sb.linear_f8_block(x, codes, scales, offsets=where, y=torch.zeros_like(y))
+        assert torch.equal(y, eager), "replay %d" % i
+
+
+def test_experts_behind_four_gib():
+    """Weights, codes and gradients of the last experts lie behind 2^32 bytes: each expert's results are those of its own weight."""
+    experts, m, n = 5, 16384, 16384
+    # Values of one binary digit, and scales of one: nothing is dropped, and sums of up to 2^15 of them are exact.
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    w = torch.empty(experts, m, n, dtype=torch.bfloat16, device=DEV)
+    for e in range(experts):
+        w[e] = torch.randint(-1, 2, (m, n), generator=gen, device=DEV, dtype=torch.int8)
+    codes, scales, codes_t, scales_t = sb.quantize_weight_f8_block(w, E4M3)
+    for e in (0, experts - 1):
+        alone = sb.quantize_weight_f8_block(w[e], E4M3)
+        assert all(torch.equal(t[e], one) for t, one in zip((codes, scales, codes_t, scales_t), alone))
+    for counts in ([3, 0, 0, 2, 4], [100, 20, 0, 60, 300]):
+        b = sum(counts)
+        where = torch.tensor([sum(counts[:e]) for e in range(experts + 1)], dtype=torch.int32, device=DEV)
+        x = torch.randint(-1, 2, (b, n), generator=gen, device=DEV, dtype=torch.int8).bfloat16()
+        y = sb.linear_f8_block(x, codes, scales, offsets=where, y_dtype=torch.float32)
+        dx = sb.linear_f8_block(x, codes_t, scales_t, offsets=where, y_dtype=torch.float32)
+        dw = sb.backward_weight_experts(x, x, where, dw_dtype=torch.float32)
+        for e in range(experts):
+            rows = slice(int(where[e]), int(where[e + 1]))
+            for got, weight in ((y, w[e]), (dx, w[e].t().contiguous())):
+                assert torch.equal(got[rows], x[rows].float() @ weight.float().t()), "expert %d of %s" % (e, counts)
+            assert torch.equal(dw[e, -512:], x[rows, -512:].float().t() @ x[rows].float()), "gradient of expert %d of %s" % (e, counts)

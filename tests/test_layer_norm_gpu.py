@@ -181,3 +181,19 @@ def test_captured_in_a_graph():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(replayed, bufs)), "replay %d" % i
+
+
+def test_rows_behind_four_gib():
+    """The last of 2.6e9 elements: their results are those of the last rows alone."""
+    b, n, last = 640000, 4096, 700
+    x = torch.randn(b, n, dtype=torch.bfloat16, device=DEV, generator=torch.Generator(device=DEV).manual_seed(6))
+    gamma, beta = torch.rand(n, device=DEV), torch.rand(n, device=DEV)
+    y, mean, rstd = sb.layer_norm(x, gamma, beta)
+    end = sb.layer_norm(x[-last:], gamma, beta)
+    assert all(torch.equal(p[-last:], q) for p, q in zip((y, mean, rstd), end))
+    y.zero_()  # dy of all rows but the last ones: dgamma and dbeta are theirs
+    dy = y
+    dy[-last:] = x[:last]
+    dx, dgamma, dbeta = sb.layer_norm_backward(dy, x, mean, rstd, gamma)
+    assert not dx[:-last].any()
+    check_backward(dy[-last:].cpu(), x[-last:].cpu(), mean[-last:].cpu(), rstd[-last:].cpu(), gamma.cpu(), dx[-last:], dgamma, dbeta)

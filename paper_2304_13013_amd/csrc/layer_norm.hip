@@ -26,51 +26,71 @@ __device__ __forceinline__ float widen(T v) {
     if constexpr (sizeof(T) == 2) return bf16_bits_to_float(v);
     else return v;
 }
-// Element type T is u16 (bf16 bits) or float; a piece is V consecutive elements: 16 bytes, or one element where rows are not
-// multiples of that.
+// Element type T is u16 (bf16 bits) or float; a piece is V consecutive elements: 16 bytes, or one element of rows shorter than
+// that.  Rows that are not whole pieces (WHOLE false) start anywhere, and their last piece starts early enough to end with the
+// row: it shares elements with the one before, which count once in the sums and are stored twice, with the same value.  (With
+// loads of single elements instead, 4000 x 1001 bf16: 6.6 us forward, 19.6 backward; @@ so.)
 template <class T, int V>
 struct Piece {
     T e[V];
 };
+typedef unsigned int v4u_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int v4u_at4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int ALIGN, bool ONCE>
+__device__ __forceinline__ v4u load_quad(const void *at) {
+    auto load = [](auto *from) -> v4u { return ONCE ? __builtin_nontemporal_load(from) : *from; };
+    if constexpr (ALIGN == 2) return load(static_cast<const v4u_at2 *>(at));
+    else if constexpr (ALIGN == 4) return load(static_cast<const v4u_at4 *>(at));
+    else return load(static_cast<const v4u *>(at));
+}
+template <int ALIGN>
+__device__ __forceinline__ void store_quad(void *at, v4u v) {
+    if constexpr (ALIGN == 2) *static_cast<v4u_at2 *>(at) = v;
+    else if constexpr (ALIGN == 4) *static_cast<v4u_at4 *>(at) = v;
+    else *static_cast<v4u *>(at) = v;
+}
 // ONCE: nobody reads it again.
-template <class T, int V, bool ONCE = true>
+template <class T, int V, bool WHOLE, bool ONCE = true>
 __device__ __forceinline__ Piece<T, V> load_piece(const T *at) {
     if constexpr (V == 1) {
         return Piece<T, 1>{{ONCE ? __builtin_nontemporal_load(at) : *at}};
     } else {
         static_assert(sizeof(T) * V == 16, "16 bytes");
-        const v4u *from = reinterpret_cast<const v4u *>(at);
-        return __builtin_bit_cast(Piece<T, V>, ONCE ? __builtin_nontemporal_load(from) : *from);
+        return __builtin_bit_cast(Piece<T, V>, (load_quad<WHOLE ? 16 : (int)sizeof(T), ONCE>(at)));
     }
 }
-template <class T, int V>
+template <class T, int V, bool WHOLE>
 __device__ __forceinline__ void store_piece(T *at, const float (&v)[V]) {
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (V == 4) *reinterpret_cast<v4f *>(at) = v4f{v[0], v[1], v[2], v[3]};
-        else *at = v[0];
+    constexpr int ALIGN = WHOLE ? 16 : (int)sizeof(T);
+    if constexpr (V == 1) {
+        if constexpr (sizeof(T) == 4) *at = v[0];
+        else *at = __builtin_bit_cast(u16, (__bf16)v[0]);
+    } else if constexpr (sizeof(T) == 4) {
+        store_quad<ALIGN>(at, __builtin_bit_cast(v4u, (v4f{v[0], v[1], v[2], v[3]})));
     } else {
-        if constexpr (V == 8) {
-            const v2u lo = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[0], v[1], v[2], v[3]}, v4bf));
-            const v2u hi = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[4], v[5], v[6], v[7]}, v4bf));
-            *reinterpret_cast<v4u *>(at) = v4u{lo.x, lo.y, hi.x, hi.y};
-        } else {
-            *at = __builtin_bit_cast(u16, (__bf16)v[0]);
-        }
+        const v2u lo = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[0], v[1], v[2], v[3]}, v4bf));
+        const v2u hi = __builtin_bit_cast(v2u, __builtin_convertvector(v4f{v[4], v[5], v[6], v[7]}, v4bf));
+        store_quad<ALIGN>(at, v4u{lo.x, lo.y, hi.x, hi.y});
     }
 }
-// V elements of a binary32 vector; `at` is as aligned as the piece of the row that it goes with.
-template <int V>
+// V elements of a binary32 vector.
+template <int V, bool WHOLE>
 __device__ __forceinline__ void load_vector(const float *v, int at, float (&out)[V]) {
     if constexpr (V == 1) {
         out[0] = v[at];
     } else {
 #pragma unroll
         for (int q = 0; q < V; q += 4) {
-            const v4f x = *reinterpret_cast<const v4f *>(v + at + q);
+            const v4f x = __builtin_bit_cast(v4f, (load_quad<WHOLE ? 16 : 4, false>(v + at + q)));
 #pragma unroll
             for (int e = 0; e < 4; ++e) out[q + e] = x[e];
         }
     }
+}
+// The piece whose columns begin at c: its first column in memory, and how many of its elements belong to the one before.
+template <int V, bool WHOLE>
+__device__ __forceinline__ int piece_at(int c, int cols) {
+    return WHOLE || V == 1 ? c : min(c, cols - V);
 }
 
 // A row belongs to a group of LANES lanes: part of a wave, a wave, or a workgroup.
@@ -102,7 +122,7 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*shared)[2][16]
 }
 
 // Rows of up to LANES * V * P columns; P pieces a lane.  mean and rstd may be null, and gamma and beta.
-template <class T, int V, int P, int LANES>
+template <class T, int V, int P, int LANES, bool WHOLE>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
                                                                             const float *__restrict__ beta, float eps,
                                                                             int64_t rows, int cols, T *__restrict__ y,
@@ -112,14 +132,17 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
     const int lane = threadIdx.x % G::LANES;
     const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)gridDim.x * G::PER_BLOCK;
     float g[P][V], b[P][V];
+    int at[P], shared_with[P];  // of a piece: first column; elements of the one before
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int c = (lane + p * G::LANES) * V;
+        at[p] = piece_at<V, WHOLE>(c, cols);
+        shared_with[p] = c - at[p];
 #pragma unroll
         for (int e = 0; e < V; ++e) g[p][e] = 1.0f, b[p][e] = 0.0f;
         if (c < cols) {
-            if (gamma != nullptr) load_vector<V>(gamma, c, g[p]);
-            if (beta != nullptr) load_vector<V>(beta, c, b[p]);
+            if (gamma != nullptr) load_vector<V, WHOLE>(gamma, at[p], g[p]);
+            if (beta != nullptr) load_vector<V, WHOLE>(beta, at[p], b[p]);
         }
     }
     Piece<T, V> raw[P];
@@ -128,7 +151,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
         for (int p = 0; p < P; ++p) {
             const int c = (lane + p * G::LANES) * V;
             raw[p] = Piece<T, V>{};
-            if (c < cols) raw[p] = load_piece<T, V>(x + row * cols + c);
+            if (c < cols) raw[p] = load_piece<T, V, WHOLE>(x + row * cols + at[p]);
         }
     };
     const float inv = 1.0f / (float)cols;
@@ -141,7 +164,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 v[p][e] = widen(raw[p].e[e]);
-                s[0] += v[p][e];
+                s[0] += WHOLE || e >= shared_with[p] ? v[p][e] : 0.0f;
             }
         if (row + step < rows) request(row + step);
         group_sums<LANES, 1>(s, shared, 0);
@@ -153,7 +176,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 v[p][e] = in ? v[p][e] - mu : 0.0f;
-                s[0] = fmaf(v[p][e], v[p][e], s[0]);
+                const float d = WHOLE || e >= shared_with[p] ? v[p][e] : 0.0f;
+                s[0] = fmaf(d, d, s[0]);
             }
         }
         group_sums<LANES, 1>(s, shared, 1);
@@ -168,13 +192,13 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = fmaf(v[p][e] * r, g[p][e], b[p][e]);
-            if (c < cols) store_piece<T, V>(y + row * cols + c, out);
+            if (c < cols) store_piece<T, V, WHOLE>(y + row * cols + at[p], out);
         }
     }
 }
 
 // Rows that do not fit: three passes, of which two find the row in L2.
-template <class T, int V>
+template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
                                                                const float *__restrict__ beta, float eps, int64_t rows, int cols,
                                                                T *__restrict__ y, float *__restrict__ mean,
@@ -185,18 +209,20 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
         const T *xr = x + row * cols;
         float s[1] = {0.0f};
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
-            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+            const int at = piece_at<V, WHOLE>(c, cols);
+            const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at);
 #pragma unroll
-            for (int e = 0; e < V; ++e) s[0] += widen(q.e[e]);
+            for (int e = 0; e < V; ++e) s[0] += at + e >= c ? widen(q.e[e]) : 0.0f;
         }
         group_sums<1024, 1>(s, shared, 0);
         const float mu = s[0] * inv;
         s[0] = 0.0f;
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
-            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+            const int at = piece_at<V, WHOLE>(c, cols);
+            const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = widen(q.e[e]) - mu;
+                const float d = at + e >= c ? widen(q.e[e]) - mu : 0.0f;
                 s[0] = fmaf(d, d, s[0]);
             }
         }
@@ -207,15 +233,16 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
             if (rstd != nullptr) rstd[row] = r;
         }
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
-            const Piece<T, V> q = load_piece<T, V, false>(xr + c);
+            const int at = piece_at<V, WHOLE>(c, cols);
+            const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at);
             float g[V], b[V], out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = 1.0f, b[e] = 0.0f;
-            if (gamma != nullptr) load_vector<V>(gamma, c, g);
-            if (beta != nullptr) load_vector<V>(beta, c, b);
+            if (gamma != nullptr) load_vector<V, WHOLE>(gamma, at, g);
+            if (beta != nullptr) load_vector<V, WHOLE>(beta, at, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = fmaf((widen(q.e[e]) - mu) * r, g[e], b[e]);
-            store_piece<T, V>(y + row * cols + c, out);
+            store_piece<T, V, WHOLE>(y + row * cols + at, out);
         }
     }
 }
@@ -264,7 +291,7 @@ __device__ __forceinline__ void column_sums(const T *__restrict__ dy, const T *_
 // row_blocks on form the sums of 16 columns each from the rows themselves: for few rows, which lie in L2 and are read twice
 // sooner than a second launch starts.  gamma lies in LDS, four consecutive elements of a lane at a time and lanes side by side:
 // in registers, next to the sums and two rows, it would leave one wave per SIMD.
-template <class T, int V, int P, int LANES, bool SUMS>
+template <class T, int V, int P, int LANES, bool SUMS, bool WHOLE>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_kernel(
     const T *__restrict__ dy, const T *__restrict__ x, const float *__restrict__ mean, const float *__restrict__ rstd,
     const float *__restrict__ gamma, int64_t rows, int cols, T *__restrict__ dx, float *__restrict__ partial, int row_blocks,
@@ -281,16 +308,24 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
     const int lane = threadIdx.x % G::LANES;
     const int64_t first = (int64_t)blockIdx.x * G::PER_BLOCK + threadIdx.x / G::LANES, step = (int64_t)(SUMS ? gridDim.x : row_blocks) * G::PER_BLOCK;
     float dg[SUMS ? P : 1][V], db[SUMS ? P : 1][V];
+    int at[P], shared_with[P];  // of a piece: first column; elements of the one before
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        at[p] = piece_at<V, WHOLE>((lane + p * G::LANES) * V, cols);
+        shared_with[p] = (lane + p * G::LANES) * V - at[p];
+    }
     if (threadIdx.x < G::LANES) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int q = 0; q < V / Q; ++q) {
-                const int c = (lane + p * G::LANES) * V + q * Q;
+                float v[Q];
+#pragma unroll
+                for (int e = 0; e < Q; ++e) v[e] = 1.0f;
+                if ((lane + p * G::LANES) * V < cols && gamma != nullptr) load_vector<Q, WHOLE>(gamma, at[p] + q * Q, v);
                 Quad g;
 #pragma unroll
-                for (int e = 0; e < Q; ++e) g[e] = 1.0f;
-                if (c < cols && gamma != nullptr) g = *reinterpret_cast<const Quad *>(gamma + c);
+                for (int e = 0; e < Q; ++e) g[e] = v[e];
                 weights[p][q][lane] = g;
             }
     }
@@ -307,8 +342,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
             const int c = (lane + p * G::LANES) * V;
             rx[p] = rdy[p] = Piece<T, V>{};
             if (c < cols) {
-                rx[p] = load_piece<T, V>(x + row * cols + c);
-                rdy[p] = load_piece<T, V>(dy + row * cols + c);
+                rx[p] = load_piece<T, V, WHOLE>(x + row * cols + at[p]);
+                rdy[p] = load_piece<T, V, WHOLE>(dy + row * cols + at[p]);
             }
         }
         mu = mean[row];
@@ -328,12 +363,12 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
             for (int e = 0; e < V; ++e) {
                 d[p][e] = widen(rdy[p].e[e]);  // zero past the last column
                 h[p][e] = in ? (widen(rx[p].e[e]) - mu) * r : 0.0f;
-                const float a = d[p][e] * weights[p][e / Q][lane][e % Q];
+                const float own = WHOLE || e >= shared_with[p] ? d[p][e] : 0.0f, a = own * weights[p][e / Q][lane][e % Q];
                 s[0] += a;
                 s[1] = fmaf(a, h[p][e], s[1]);
                 if (SUMS) {
-                    dg[p][e] = fmaf(d[p][e], h[p][e], dg[p][e]);
-                    db[p][e] += d[p][e];
+                    dg[p][e] = fmaf(own, h[p][e], dg[p][e]);
+                    db[p][e] += own;
                 }
             }
         }
@@ -346,7 +381,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
             float out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = r0 * (fmaf(d[p][e], weights[p][e / Q][lane][e % Q], -sa) - h[p][e] * sh);
-            if (c < cols) store_piece<T, V>(dx + row * cols + c, out);
+            if (c < cols) store_piece<T, V, WHOLE>(dx + row * cols + at[p], out);
         }
     }
     if constexpr (SUMS) {
@@ -356,8 +391,9 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const int c = (lane + p * G::LANES) * V + e;
-                    if (c < cols) mine[c] = dg[p][e], mine[cols + c] = db[p][e];
+                    const int c = at[p] + e;
+                    if (c < cols && (WHOLE || ((lane + p * G::LANES) * V < cols && e >= shared_with[p])))
+                        mine[c] = dg[p][e], mine[cols + c] = db[p][e];
                 }
         } else {
             // The waves' sums of a piece at a time, in wave order.
@@ -369,8 +405,10 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
                 __syncthreads();
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    meet[wave][0][e * G::LANES + lane] = dg[p][e];
-                    meet[wave][1][e * G::LANES + lane] = db[p][e];
+                    // What is shared with the piece before is zero, and goes behind the last column.
+                    const int to = WHOLE ? e : (e - shared_with[p]) & (V - 1);
+                    meet[wave][0][to * G::LANES + lane] = dg[p][e];
+                    meet[wave][1][to * G::LANES + lane] = db[p][e];
                 }
                 __syncthreads();
                 for (int i = threadIdx.x; i < 2 * SLOTS; i += G::THREADS) {
@@ -388,7 +426,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_backward_ker
 }
 
 // Rows that do not fit: two passes; the sums over the rows are another launch's.
-template <class T, int V>
+template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T *__restrict__ dy, const T *__restrict__ x,
                                                                         const float *__restrict__ mean,
                                                                         const float *__restrict__ rstd,
@@ -402,14 +440,15 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T 
         const float mu = mean[row], r = rstd[row];
         float s[2] = {0.0f, 0.0f};
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
-            const Piece<T, V> q = load_piece<T, V, false>(xr + c), d = load_piece<T, V, false>(dr + c);
+            const int at = piece_at<V, WHOLE>(c, cols);
+            const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at), d = load_piece<T, V, WHOLE, false>(dr + at);
             float g[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = 1.0f;
-            if (gamma != nullptr) load_vector<V>(gamma, c, g);
+            if (gamma != nullptr) load_vector<V, WHOLE>(gamma, at, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float a = widen(d.e[e]) * g[e];
+                const float a = at + e >= c ? widen(d.e[e]) * g[e] : 0.0f;
                 s[0] += a;
                 s[1] = fmaf(a, (widen(q.e[e]) - mu) * r, s[1]);
             }
@@ -417,14 +456,15 @@ __global__ __launch_bounds__(1024) void layer_norm_backward_long_kernel(const T 
         group_sums<1024, 2>(s, shared, turn);
         const float sa = s[0] * inv, sh = s[1] * inv;
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
-            const Piece<T, V> q = load_piece<T, V, false>(xr + c), d = load_piece<T, V, false>(dr + c);
+            const int at = piece_at<V, WHOLE>(c, cols);
+            const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at), d = load_piece<T, V, WHOLE, false>(dr + at);
             float g[V], out[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) g[e] = 1.0f;
-            if (gamma != nullptr) load_vector<V>(gamma, c, g);
+            if (gamma != nullptr) load_vector<V, WHOLE>(gamma, at, g);
 #pragma unroll
             for (int e = 0; e < V; ++e) out[e] = r * (widen(d.e[e]) * g[e] - sa - (widen(q.e[e]) - mu) * r * sh);
-            store_piece<T, V>(dx + row * cols + c, out);
+            store_piece<T, V, WHOLE>(dx + row * cols + at, out);
         }
     }
 }
@@ -487,9 +527,9 @@ int walkers(int64_t rows, int per_block, int per_cu) {
 }
 
 // The group and the pieces for rows of `cols` columns, V elements a piece: calls f(integral constants P, LANES), or returns
-// false for rows that do not fit.  A lane holds at most 32 elements; eight waves only of whole pieces (the others' 32 addresses
-// would not fit in its registers), parts of a wave too (rows of single elements would be many loads).
-template <int V, class F>
+// false for rows that do not fit.  A lane holds at most 32 elements; eight waves only of whole pieces (the others' columns and
+// masks would not fit in its registers).
+template <int V, bool WHOLE, class F>
 bool with_group(int cols, F f) {
     auto go = [&](auto elements, auto lanes) {
         constexpr int E = decltype(elements)::value, L = decltype(lanes)::value;
@@ -504,34 +544,42 @@ bool with_group(int cols, F f) {
     typedef std::integral_constant<int, 64> Wave;
     typedef std::integral_constant<int, 256> FourWaves;
     typedef std::integral_constant<int, 512> EightWaves;
-    if constexpr (V > 1) {
-        if (go(E8(), std::integral_constant<int, 8>()) || go(E8(), std::integral_constant<int, 16>()) || go(E8(), std::integral_constant<int, 32>()))
-            return true;
+    if constexpr (V == 1) {
+        return go(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());  // shorter than a piece
+    } else {
+        const bool done = go(E8(), std::integral_constant<int, 8>()) || go(E8(), std::integral_constant<int, 16>()) ||
+                          go(E8(), std::integral_constant<int, 32>()) || go(E8(), Wave()) || go(E16(), Wave()) ||
+                          go(E24(), Wave()) || go(E32(), Wave()) || go(E16(), FourWaves()) || go(E32(), FourWaves());
+        if constexpr (WHOLE) return done || go(E32(), EightWaves());
+        return done;
     }
-    const bool done = go(E8(), Wave()) || go(E16(), Wave()) || go(E24(), Wave()) || go(E32(), Wave()) || go(E16(), FourWaves()) ||
-                      go(E32(), FourWaves());
-    if constexpr (V > 1) return done || go(E32(), EightWaves());
-    return done;
 }
-// Columns of the longest rows that fit.
-int longest_row(bool whole) { return whole ? 16384 : 8192; }
+int longest_row(bool whole) { return whole ? 16384 : 8192; }  // that fits
 
-template <class T, int V>
+// f(pieces of V elements, whether rows are whole pieces)
+template <int V, class F>
+hipError_t with_pieces(int64_t cols, F f) {
+    if (cols % V == 0) return f(std::integral_constant<int, V>(), std::true_type());
+    if (cols >= V) return f(std::integral_constant<int, V>(), std::false_type());
+    return f(std::integral_constant<int, 1>(), std::true_type());
+}
+
+template <class T, int V, bool WHOLE>
 hipError_t forward_of(const T *x, const float *gamma, const float *beta, float eps, int64_t rows, int cols, T *y, float *mean,
                       float *rstd, hipStream_t stream) {
-    const bool fits = with_group<V>(cols, [&](auto pieces, auto lanes) {
+    const bool fits = with_group<V, WHOLE>(cols, [&](auto pieces, auto lanes) {
         constexpr int P = decltype(pieces)::value, L = decltype(lanes)::value;
         typedef Group<L> G;
-        layer_norm_kernel<T, V, P, L><<<walkers(rows, G::PER_BLOCK, L == 512 ? 4 : 8), G::THREADS, 0, stream>>>(
+        layer_norm_kernel<T, V, P, L, WHOLE><<<walkers(rows, G::PER_BLOCK, L == 512 ? 4 : 8), G::THREADS, 0, stream>>>(
             x, gamma, beta, eps, rows, cols, y, mean, rstd);
     });
     if (!fits)
-        layer_norm_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(x, gamma, beta, eps, rows, cols, y, mean, rstd);
+        layer_norm_long_kernel<T, V, WHOLE><<<walkers(rows, 1, 2), 1024, 0, stream>>>(x, gamma, beta, eps, rows, cols, y, mean, rstd);
     return hipGetLastError();
 }
 
 // Rows that a workgroup works on at a time, of at most 2048 columns.
-int rows_per_block(int cols, bool whole) { return !whole || cols > 256 ? 4 : cols > 128 ? 8 : cols > 64 ? 16 : 32; }
+int rows_per_block(int cols) { return cols > 256 ? 4 : cols > 128 ? 8 : cols > 64 ? 16 : 32; }
 
 // Few rows: the sums over them in the launch of the rows, which are read twice (1200 x 768 bf16: 7.6 us, 9.5 in two launches; 600 x
 // 2048 f32 6.5 / 12.2; on the other side 1200 x 4096 f32 22.9 / 22.1, 2500 x 768 bf16 19.7 / 10.8).
@@ -549,30 +597,30 @@ int backward_blocks(int64_t rows, int cols, bool whole) {
         const int64_t four = (rows + 3) / 4;
         return (int)(four < num_compute_units() ? four : num_compute_units());
     }
-    const int per_block = rows_per_block(cols, whole);
+    const int per_block = rows_per_block(cols);
     return walkers(rows, per_block, rows >= (int64_t)4 * per_block * num_compute_units() ? 2 : 1);
 }
 
-template <class T, int V>
+template <class T, int V, bool WHOLE>
 hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *rstd, const float *gamma, int64_t rows, int cols,
                        T *dx, float *dgamma, float *dbeta, float *partial, hipStream_t stream) {
-    const bool any = dgamma != nullptr || dbeta != nullptr, one_launch = sums_in_one_launch(rows, cols, V > 1), sums = any && !one_launch;
-    const int blocks = backward_blocks(rows, cols, V > 1);
+    const bool any = dgamma != nullptr || dbeta != nullptr, one_launch = sums_in_one_launch(rows, cols, WHOLE), sums = any && !one_launch;
+    const int blocks = backward_blocks(rows, cols, WHOLE);
     if (rows > 0) {
-        const bool fits = with_group<V>(cols, [&](auto pieces, auto lanes) {
+        const bool fits = with_group<V, WHOLE>(cols, [&](auto pieces, auto lanes) {
             constexpr int P = decltype(pieces)::value, L = decltype(lanes)::value;
             typedef Group<L> G;
             if (sums)
-                layer_norm_backward_kernel<T, V, P, L, true><<<blocks, G::THREADS, 0, stream>>>(
+                layer_norm_backward_kernel<T, V, P, L, true, WHOLE><<<blocks, G::THREADS, 0, stream>>>(
                     dy, x, mean, rstd, gamma, rows, cols, dx, partial, 0, nullptr, nullptr);
             else {
                 const int row_blocks = walkers(rows, G::PER_BLOCK, 4);
-                layer_norm_backward_kernel<T, V, P, L, false><<<row_blocks + (any ? (cols + 15) / 16 : 0), G::THREADS, 0, stream>>>(
+                layer_norm_backward_kernel<T, V, P, L, false, WHOLE><<<row_blocks + (any ? (cols + 15) / 16 : 0), G::THREADS, 0, stream>>>(
                     dy, x, mean, rstd, gamma, rows, cols, dx, nullptr, row_blocks, dgamma, dbeta);
             }
         });
         if (!fits) {
-            layer_norm_backward_long_kernel<T, V><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);
+            layer_norm_backward_long_kernel<T, V, WHOLE><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);
             if (sums)
                 layer_norm_column_sums_kernel<T><<<dim3((cols + 255) / 256, kLongParts), 256, 0, stream>>>(dy, x, mean, rstd, rows,
                                                                                                           cols, partial);
@@ -584,8 +632,6 @@ hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *
         layer_norm_reduce_kernel<<<(2 * cols + 15) / 16, 1024, 0, stream>>>(partial, rows > 0 ? blocks : 0, cols, dgamma, dbeta);
     return hipGetLastError();
 }
-
-bool whole_pieces(int64_t cols, bool bf16) { return cols % (bf16 ? 8 : 4) == 0; }
 
 }  // namespace
 
@@ -599,34 +645,26 @@ size_t layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
 
 hipError_t launch_layer_norm(const void *x, const float *gamma, const float *beta, float eps, int64_t rows, int64_t cols, bool bf16,
                              void *y, float *mean, float *rstd, hipStream_t stream) {
-    const bool whole = whole_pieces(cols, bf16);
-    if (bf16) {
-        const u16 *xs = static_cast<const u16 *>(x);
-        u16 *ys = static_cast<u16 *>(y);
-        return whole ? forward_of<u16, 8>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream)
-                     : forward_of<u16, 1>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream);
-    }
-    const float *xs = static_cast<const float *>(x);
-    float *ys = static_cast<float *>(y);
-    return whole ? forward_of<float, 4>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream)
-                 : forward_of<float, 1>(xs, gamma, beta, eps, rows, (int)cols, ys, mean, rstd, stream);
+    auto of = [&](auto element, auto v, auto whole) {
+        typedef decltype(element) T;
+        return forward_of<T, decltype(v)::value, decltype(whole)::value>(static_cast<const T *>(x), gamma, beta, eps, rows, (int)cols,
+                                                                         static_cast<T *>(y), mean, rstd, stream);
+    };
+    if (bf16) return with_pieces<8>(cols, [&](auto v, auto whole) { return of(u16(), v, whole); });
+    return with_pieces<4>(cols, [&](auto v, auto whole) { return of(float(), v, whole); });
 }
 
 hipError_t launch_layer_norm_backward(const void *dy, const void *x, const float *mean, const float *rstd, const float *gamma,
                                       int64_t rows, int64_t cols, bool bf16, void *dx, float *dgamma, float *dbeta, void *ws,
                                       hipStream_t stream) {
-    const bool whole = whole_pieces(cols, bf16);
-    float *partial = static_cast<float *>(ws);
-    if (bf16) {
-        const u16 *d = static_cast<const u16 *>(dy), *xs = static_cast<const u16 *>(x);
-        u16 *out = static_cast<u16 *>(dx);
-        return whole ? backward_of<u16, 8>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream)
-                     : backward_of<u16, 1>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream);
-    }
-    const float *d = static_cast<const float *>(dy), *xs = static_cast<const float *>(x);
-    float *out = static_cast<float *>(dx);
-    return whole ? backward_of<float, 4>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream)
-                 : backward_of<float, 1>(d, xs, mean, rstd, gamma, rows, (int)cols, out, dgamma, dbeta, partial, stream);
+    auto of = [&](auto element, auto v, auto whole) {
+        typedef decltype(element) T;
+        return backward_of<T, decltype(v)::value, decltype(whole)::value>(static_cast<const T *>(dy), static_cast<const T *>(x), mean, rstd,
+                                                                          gamma, rows, (int)cols, static_cast<T *>(dx), dgamma, dbeta,
+                                                                          static_cast<float *>(ws), stream);
+    };
+    if (bf16) return with_pieces<8>(cols, [&](auto v, auto whole) { return of(u16(), v, whole); });
+    return with_pieces<4>(cols, [&](auto v, auto whole) { return of(float(), v, whole); });
 }
 
 }  // namespace sb

@@ -29,7 +29,7 @@ __device__ __forceinline__ float widen(T v) {
 // Element type T is u16 (bf16 bits) or float; a piece is V consecutive elements: 16 bytes, or one element of rows shorter than
 // that.  Rows that are not whole pieces (WHOLE false) start anywhere, and their last piece starts early enough to end with the
 // row: it shares elements with the one before, which count once in the sums and are stored twice, with the same value.  (With
-// loads of single elements instead, 4000 x 1001 bf16: 6.6 us forward, 19.6 backward; @@ so.)
+// loads of single elements instead, 4000 x 1001 bf16: 6.8 us forward, 19.7 backward; 5.9 and 13.8 so.)
 template <class T, int V>
 struct Piece {
     T e[V];

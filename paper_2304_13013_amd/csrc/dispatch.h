@@ -216,6 +216,7 @@ inline int plan_few_runs(int64_t M, int64_t experts) {
 struct ExpertProductPlan {
     TileKind rest;
     int split, runs;
+    int cut;  // 256x256 tiles: the tiled kernel's workgroups, if tile rows behind its last whole round go to the small-product kernel
 };
 inline ExpertProductPlan plan_expert_product(int64_t M, int64_t N, int64_t K, int64_t experts, int out_bytes, int ncu) {
     const int64_t used = experts < M ? experts : M;
@@ -223,7 +224,7 @@ inline ExpertProductPlan plan_expert_product(int64_t M, int64_t N, int64_t K, in
         const int64_t even = (M + rows / 2 * used + rows - 1) / rows;
         return even > used ? even : used;
     };
-    ExpertProductPlan plan{TILES_256, DIRECT_NONE, 0};
+    ExpertProductPlan plan{TILES_256, DIRECT_NONE, 0, 0};
     double best = tiles_time(TILES_256, row_blocks(256) * ((N + 255) / 256), M, N, K, PRODUCT_F8, out_bytes, ncu);
     const double narrow = tiles_time(TILES_256X128, row_blocks(256) * ((N + 127) / 128), M, N, K, PRODUCT_F8, out_bytes, ncu);
     if (narrow < best) {
@@ -238,6 +239,20 @@ inline ExpertProductPlan plan_expert_product(int64_t M, int64_t N, int64_t K, in
         const int64_t rows = split == DIRECT_32 ? 32 : 64, runs = (2 * ((M + experts - 1) / experts) + rows - 1) / rows;
         plan.split = split;
         plan.runs = (int)(runs < 64 ? runs : 64);
+        return plan;
+    }
+    // Tiles that hardly begin a round of long ones: how many there are is seen on the GPU, where the estimate decides again (8
+    // experts, 4096 -> 1024: 16448 rows 81-87 us on 256x128 tiles, 64-68 so; 33500 rows 151 / 124-136; 8192 -> 1024, 17000 rows
+    // 158 / 128).  Not where the experts' cut tile rows are so many that the estimate says little.
+    const int64_t tiles_n = (N + 255) / 256, tiles = row_blocks(256) * tiles_n, rest = tiles % ncu;
+    if (tiles > ncu && rest <= ncu / 8 && experts * tiles_n <= ncu / 4) {
+        const int64_t last = (rest + tiles_n - 1) / tiles_n * 4 * (N / 64);
+        const double cut = tiles_time(TILES_256, tiles - rest, M, N, K, PRODUCT_F8, out_bytes, ncu) + 3.0 +
+                           direct_blocks_time(4 * last, last, K, ncu, &split);
+        if (cut < 0.95 * best) {
+            plan.rest = TILES_256;
+            plan.cut = ncu;
+        }
     }
     return plan;
 }

@@ -14,9 +14,14 @@ typedef DirectCfg<64, 64, 2> D64H;
 typedef BlockWideCfg<256> W256;
 typedef BlockWideCfg<128> W128;
 
+struct Rest64 : D64 {};  // D64 on what the tiled kernel leaves
 template <class C, int OUT, int FA, int FB>
 struct Body {
     static __device__ __forceinline__ void run(const GemmBlockArgs &p) { gemm_f8_block_direct_body<C, OUT, FA, FB>(p); }
+};
+template <int OUT, int FA, int FB>
+struct Body<Rest64, OUT, FA, FB> {
+    static __device__ __forceinline__ void run(const GemmBlockArgs &p) { gemm_f8_block_direct_body<D64, OUT, FA, FB, true>(p); }
 };
 template <int BN, int OUT, int FA, int FB>
 struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
@@ -31,6 +36,7 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
 #define WAVES_D32
 #define WAVES_D64
 #define WAVES_D64H
+#define WAVES_Rest64
 #define WAVES_W256 __attribute__((amdgpu_waves_per_eu(1, 1)))  // one wave per SIMD: all 512 registers are a lane's
 #define WAVES_W128 __attribute__((amdgpu_waves_per_eu(1, 1)))
 // name suffix: format of the token-side operand, then of the weight-side operand (4 = E4M3, 5 = E5M2)
@@ -46,6 +52,7 @@ struct Body<BlockWideCfg<BN>, OUT, FA, FB> {
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d32, D32)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d64, D64)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_d64h, D64H)
+SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_rest, Rest64)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_n, W128)
 SB_BLOCK_ENTRIES(SB_BLOCK_ENTRY, gemm_f8b_w, W256)
 SB_BLOCK_ENTRIES(SB_FEW_ENTRY, gemm_f8b_few, FewCfg)
@@ -58,9 +65,9 @@ typedef void (*FewKernel)(GemmFewArgs);
 #define SB_BLOCK_ROW(name)                                                                                          \
     {name##_a4b4_bf16, name##_a4b4_f32, name##_a5b4_bf16, name##_a5b4_f32, name##_a4b5_bf16, name##_a4b5_f32,       \
      name##_a5b5_bf16, name##_a5b5_f32}
-enum { K_D32, K_D64, K_D64H, K_N, K_W, KERNELS };
+enum { K_D32, K_D64, K_D64H, K_REST, K_N, K_W, KERNELS };
 const Kernel kernels[KERNELS][8] = {SB_BLOCK_ROW(gemm_f8b_d32), SB_BLOCK_ROW(gemm_f8b_d64), SB_BLOCK_ROW(gemm_f8b_d64h),
-                                    SB_BLOCK_ROW(gemm_f8b_n), SB_BLOCK_ROW(gemm_f8b_w)};
+                                    SB_BLOCK_ROW(gemm_f8b_rest), SB_BLOCK_ROW(gemm_f8b_n), SB_BLOCK_ROW(gemm_f8b_w)};
 const FewKernel few_kernels[8] = SB_BLOCK_ROW(gemm_f8b_few);
 #undef SB_BLOCK_ROW
 std::atomic<bool> lds_set[KERNELS][8];  // zero-initialized; a racing second set is harmless
@@ -127,6 +134,7 @@ hipError_t launch_gemm_f8_block_few(const void *x, int64_t cols, int fmt_x, cons
     args.K = (int)((cols + 127) / 128 * 128);
     args.sa_rows = args.sa_bytes = 0;
     args.runs = plan_few_runs(M, experts);
+    args.cut = 0;
     args.experts = (int)experts;
     args.cols = (int)cols;
     const int which = (fmt_b ? 4 : 0) + (fmt_x ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);
@@ -157,13 +165,16 @@ hipError_t launch_gemm_f8_block(const uint8_t *aq, int fmt_a, const uint8_t *sca
     args.sa_rows = (int)M;
     args.sa_bytes = (int)(uint32_t)((K / 128 + 3) / 4 * M * 4);
     args.experts = (int)experts;
-    args.runs = 0;
+    args.runs = args.cut = 0;
     const int which = (fmt_b ? 4 : 0) + (fmt_a ? 2 : 0) + (out_dtype == SB_BF16 ? 0 : 1);
     const int ncu = num_compute_units(), out_bytes = out_dtype == SB_BF16 ? 2 : 4;
     if (offsets != nullptr) {
         const ExpertProductPlan plan = plan_expert_product(M, N, K, experts, out_bytes, ncu);
         if (plan.split != DIRECT_NONE) return launch_direct(plan.split, plan.runs, which, args, stream);
-        return launch_tiled(plan.rest, M / 256 + experts, which, args, stream);
+        args.cut = plan.cut;
+        const hipError_t e = launch_tiled(plan.rest, M / 256 + experts, which, args, stream);
+        if (e != hipSuccess || plan.cut == 0) return e;
+        return launch(K_REST, which, ncu, D64::THREADS, BlockDirect<D64>::LDS_BYTES, args, stream);
     }
     const ProductPlan plan = plan_product(M, N, K, PRODUCT_F8, out_bytes, ncu, TILES_256X128);
     if (plan.first_rows > 0) {

@@ -28,6 +28,7 @@ struct GemmBlockArgs {
     void *out;              // [M,N]
     int M, N, K, sa_rows, sa_bytes, experts;  // sa_bytes: from sa to the end of the scales, below 2^32
     int runs;               // direct kernel: workgroups that share the row blocks of an expert and a column block
+    int cut;                // experts, 256x256 tiles: their workgroups, if a last round of few tiles is the direct kernel's; else 0
 };
 
 // Rows of an expert: [first, end).
@@ -38,6 +39,55 @@ __device__ __forceinline__ void expert_rows(const GemmBlockArgs &p, int e, int *
         *first = min(max(uniform_load(p.offsets + e), 0), p.M);
         *end = min(max(uniform_load(p.offsets + e + 1), *first), p.M);
     }
+}
+
+// The tile rows of all experts, numbered through: `before` this lane's share of the experts, `total` of all.
+struct ExpertTiles {
+    static constexpr int ROWS = 256;
+    int share, before, total;
+};
+__device__ __forceinline__ ExpertTiles expert_tiles(const GemmBlockArgs &p) {
+    ExpertTiles t{(p.experts + 63) / 64, 0, 0};
+    const int lane = threadIdx.x & 63;
+    int mine = 0;
+    for (int i = 0; i < t.share; ++i) {
+        const int e = lane * t.share + i;
+        if (e < p.experts) {
+            const int first = min(max(p.offsets[e], 0), p.M), end = min(max(p.offsets[e + 1], first), p.M);
+            mine += (end - first + ExpertTiles::ROWS - 1) / ExpertTiles::ROWS;
+        }
+    }
+    int sum = mine;  // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(sum, d, 64);
+        if (lane >= d) sum += other;
+    }
+    t.before = sum - mine;
+    t.total = __builtin_amdgcn_readlane(sum, 63);
+    return t;
+}
+// Tile row tm < total: its expert, first row and the end of the expert's rows.
+__device__ __forceinline__ void find_tile(const GemmBlockArgs &p, const ExpertTiles &t, int tm, int *expert, int *row, int *end) {
+    // The last lane that has no more than tm tile rows before its share has the tile's expert in it.
+    const int owner = __builtin_popcountll(__builtin_amdgcn_ballot_w64(t.before <= tm)) - 1;
+    int at = tm - __builtin_amdgcn_readlane(t.before, owner);
+    for (int e = owner * t.share;; ++e) {
+        int first;
+        expert_rows(p, e, &first, end);
+        const int tiles = (*end - first + ExpertTiles::ROWS - 1) / ExpertTiles::ROWS;
+        *expert = e;
+        *row = first + at * ExpertTiles::ROWS;
+        if (at < tiles || e + 1 >= p.experts) return;
+        at -= tiles;
+    }
+}
+// Tile rows that the tiled kernel works on, of `total`; the direct kernel has the others: those behind the last whole round, if
+// they are at most an eighth of a round, two rounds of its blocks (plan_expert_product; both kernels decide alike).
+__device__ __forceinline__ int tiled_rows(const GemmBlockArgs &p, int total, int tiles_n) {
+    if (p.cut == 0) return total;
+    const int tiles = total * tiles_n, whole = tiles / p.cut * p.cut;
+    return whole == 0 || tiles - whole > p.cut / 8 ? total : whole / tiles_n;
 }
 
 // Byte i of an array that starts at a multiple of 4, as part of its dword.
@@ -53,7 +103,8 @@ struct BlockDirect {  // C: DirectCfg
     static_assert(LDS_BYTES <= 160 * 1024 && C::ROWS <= 64 && C::ROWS * C::PITCH * 4 <= WAVE_BYTES, "LDS");
 };
 
-template <class C, int OUT, int FMT_A, int FMT_B>
+// REST: the tile rows that tiled_rows leaves, an item for each block of rows and columns.
+template <class C, int OUT, int FMT_A, int FMT_B, bool REST = false>
 __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p) {
     typedef BlockDirect<C> D;
     typedef __attribute__((address_space(3))) void lds_void;
@@ -62,11 +113,8 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int frow = lane & 31, fhalf = lane >> 5;
     // Workgroups of one b follow each other, its column blocks fastest: few experts' weights are in flight at a time.
-    const int cols = p.N / C::COLS, block = (int)blockIdx.x % cols, rest = (int)blockIdx.x / cols;
-    const int run = rest % p.runs, expert = rest / p.runs;
-    const int n0 = block * C::COLS;
-    int first, end;
-    expert_rows(p, expert, &first, &end);
+    const int cols = p.N / C::COLS;
+    int n0 = 0, end = 0;
     const int KB = p.K / C::BK;
     const int s0 = (int)((long long)wave * KB / C::WAVES), s1 = (int)((long long)(wave + 1) * KB / C::WAVES), n = s1 - s0;
 
@@ -74,9 +122,14 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
         __builtin_amdgcn_make_buffer_rsrc((void *)p.a, 0, (unsigned)((size_t)p.M * (size_t)p.K), 0x00020000);
     const __amdgpu_buffer_rsrc_t rsrc_sa =
         __builtin_amdgcn_make_buffer_rsrc((void *)p.sa, 0, (unsigned)p.sa_bytes, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rsrc_b = __builtin_amdgcn_make_buffer_rsrc(
-        (void *)(p.b + (int64_t)expert * p.N * p.K), 0, (unsigned)((size_t)p.N * (size_t)p.K), 0x00020000);
-    const int64_t sb_row = ((int64_t)expert * ((p.N + 127) / 128) + n0 / 128) * KB;
+    __amdgpu_buffer_rsrc_t rsrc_b;
+    int64_t sb_row = 0;
+    auto set_weight = [&](int expert, int block) {
+        n0 = block * C::COLS;
+        rsrc_b = __builtin_amdgcn_make_buffer_rsrc((void *)(p.b + (int64_t)expert * p.N * p.K), 0, (unsigned)((size_t)p.N * (size_t)p.K),
+                                                   0x00020000);
+        sb_row = ((int64_t)expert * ((p.N + 127) / 128) + n0 / 128) * KB;
+    };
     unsigned voff[2];
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
@@ -92,7 +145,7 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) frag_off[kk] = frow * C::BK + (((kk * 2 + fhalf) ^ ((frow >> 1) & 7)) << 4);
 
-    for (int m0 = first + run * C::ROWS; m0 < end; m0 += p.runs * C::ROWS) {
+    auto row_block = [&](int m0) __attribute__((always_inline)) {
         auto issue = [&](int i) {  // stage i of this wave's n: rows past M read as zero; rows of another expert are not stored
             unsigned char *dst = ring + (i % C::STAGES) * D::SLOT_BYTES;
             const unsigned k0 = (unsigned)(s0 + i) * C::BK;
@@ -212,6 +265,26 @@ __device__ __forceinline__ void gemm_f8_block_direct_body(const GemmBlockArgs &p
             }
         }
         __syncthreads();  // the next row block's requests write where the sums were read
+    };
+    if constexpr (REST) {
+        constexpr int BLOCKS = ExpertTiles::ROWS / C::ROWS;  // of a tile row
+        const ExpertTiles t = expert_tiles(p);
+        const int done = tiled_rows(p, t.total, (p.N + 255) / 256), items = (t.total - done) * BLOCKS * cols;
+        for (int item = (int)blockIdx.x; item < items; item += (int)gridDim.x) {
+            const int q = item / cols;
+            int expert, row;
+            find_tile(p, t, done + q / BLOCKS, &expert, &row, &end);
+            row += q % BLOCKS * C::ROWS;
+            if (row >= end) continue;
+            set_weight(expert, item % cols);
+            row_block(row);
+        }
+    } else {
+        const int rest = (int)blockIdx.x / cols, run = rest % p.runs, expert = rest / p.runs;
+        int first;
+        expert_rows(p, expert, &first, &end);
+        set_weight(expert, (int)blockIdx.x % cols);
+        for (int m0 = first + run * C::ROWS; m0 < end; m0 += p.runs * C::ROWS) row_block(m0);
     }
 }
 

@@ -54,7 +54,8 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
     const int KT = p.K / C::BK;
     const int tiles_n = (p.N + BN - 1) / BN, blocks_n = (p.N + 127) / 128;
 
-    // ---- Tiles.  before: tile rows of the experts before this lane's share; total: of all.
+    // ---- Tiles.  before: tile rows of the experts before this lane's share; total: of all.  (As in expert_tiles and
+    // find_tile, written out: called here, they make the compiler copy fragments that are still on their way.)
     const int share = (p.experts + 63) / 64;
     int before = 0, total = (p.M + C::BM - 1) / C::BM;
     if (p.offsets != nullptr) {
@@ -74,6 +75,7 @@ __device__ __forceinline__ void gemm_f8_block_wide_body(const GemmBlockArgs &p) 
         }
         before = sum - mine;
         total = __builtin_amdgcn_readlane(sum, 63);
+        if constexpr (BN == 256) total = tiled_rows(p, total, tiles_n);
     }
     struct Tile {
         int row, end, tn, expert;  // first row; end of the expert's rows

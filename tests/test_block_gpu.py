@@ -468,3 +468,24 @@ def test_experts_behind_four_gib():
             for got, weight in ((y, w[e]), (dx, w[e].t().contiguous())):
                 assert torch.equal(got[rows], x[rows].float() @ weight.float().t()), "expert %d of %s" % (e, counts)
             assert torch.equal(dw[e, -512:], x[rows, -512:].float().t() @ x[rows].float()), "gradient of expert %d of %s" % (e, counts)
+
+
+@pytest.mark.parametrize("counts", [[4971, 2444, 2452, 4249, 0, 0, 2332, 0], [2056] * 8, [16384, 0, 0, 0, 0, 0, 0, 64], [64, 16384, 0, 0, 0, 0, 0, 0],
+                                    [300] * 7 + [14348], [16448, 0, 0, 0, 0, 0, 0, 0], [100] * 7 + [15000]],
+                         ids=["uneven", "even", "whole", "first", "last", "one", "padded"])
+def test_last_tile_rows_of_experts(counts):
+    """A contraction of 4096 for 16448 rows of 8 experts: where the last round of tiles is nearly empty, its rows are the
+    small-product kernel's.  Values of one binary digit: every sum is exact."""
+    b, n, m, experts = 16448, 4096, 1024, 8
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    w = torch.randint(-1, 2, (experts, m, n), generator=gen, device=DEV, dtype=torch.int8).bfloat16()
+    x = torch.randint(-1, 2, (b, n), generator=gen, device=DEV, dtype=torch.int8).bfloat16()
+    where = torch.tensor([sum(counts[:e]) for e in range(experts + 1)], dtype=torch.int32, device=DEV)
+    codes, scales, _, _ = sb.quantize_weight_f8_block(w, E4M3)
+    for dtype in (torch.bfloat16, torch.float32):
+        y = torch.full((b, m), -7.0, dtype=dtype, device=DEV)
+        sb.linear_f8_block(x, codes, scales, offsets=where, y=y)
+        for e in range(experts):
+            rows = slice(int(where[e]), int(where[e + 1]))
+            assert torch.equal(y[rows], (x[rows].float() @ w[e].float().t()).to(dtype)), "expert %d" % e
+        assert (y[sum(counts):] == -7.0).all()

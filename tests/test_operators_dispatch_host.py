@@ -19,7 +19,7 @@ extern "C" void product(long long M, long long N, long long K, int out_bytes, in
 }
 extern "C" void expert_product(long long M, long long N, long long K, long long experts, int out_bytes, int ncu, long long *o) {
     const sb::ExpertProductPlan p = sb::plan_expert_product(M, N, K, experts, out_bytes, ncu);
-    o[0] = p.rest, o[1] = p.split, o[2] = p.runs;
+    o[0] = p.rest, o[1] = p.split, o[2] = p.runs, o[3] = p.cut;
 }
 extern "C" void expert_gradient(long long b, long long n, long long m, long long experts, int ncu, long long *o) {
     const sb::ExpertGradPlan p = sb::plan_expert_gradient(b, n, m, experts, ncu);
@@ -75,7 +75,7 @@ def test_plain_products_are_covered_once(plans):
 def test_expert_products_have_workgroups(plans):
     for M, N, K, E in sizes(2, 4000):
         for out_bytes in (2, 4):
-            rest, split, runs = call(plans.expert_product, 3, M, N, K, E, out_bytes, NCU)
+            rest, split, runs, _ = call(plans.expert_product, 4, M, N, K, E, out_bytes, NCU)
             assert rest in (TILES_256X128, TILES_256)
             if split != DIRECT_NONE:
                 assert 1 <= runs <= 64 and N // 32 * E * runs < 2 ** 31, (M, N, K, E)
@@ -101,3 +101,18 @@ def test_expert_gradients_have_items(plans):
     assert call(plans.expert_gradient, 2, 5003, 768, 1088, 24, NCU) == [1, 1]
     assert call(plans.expert_gradient, 2, 30000, 640, 704, 2, NCU)[1] > 1
     assert call(plans.expert_gradient, 2, 16448, 1024, 4096, 8, NCU) == [0, 1]
+
+
+def test_cut_of_expert_products(plans):
+    """Only 256x256 tiles of more than a round give their last tile rows away, and only where the experts' cut tile rows are few."""
+    cuts = 0
+    for M, N, K, E in list(sizes(11, 4000)) + [(16448, 1024, 4096, 8), (33500, 1024, 4096, 8), (17000, 1024, 8192, 8)]:
+        for out_bytes in (2, 4):
+            rest, split, _, cut = call(plans.expert_product, 4, M, N, K, E, out_bytes, NCU)
+            assert cut in (0, NCU)
+            if cut:
+                cuts += 1
+                assert rest == TILES_256 and split == DIRECT_NONE and E * -(-N // 256) <= NCU // 4 and (M / 256 + E) * -(-N // 256) > NCU
+    assert cuts >= 6
+    assert call(plans.expert_product, 4, 16448, 1024, 4096, 8, 2, NCU)[3] == NCU
+    assert call(plans.expert_product, 4, 16448, 4096, 1024, 8, 2, NCU)[3] == 0

@@ -825,13 +825,13 @@ def layer_norm(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None)
     latter f32 [rows], as layer_norm_backward takes them."""
     lib = _entries()
     rows, cols = x.shape
-    dtype = _rows_dtype(x)
-    y = _out(y, (rows, cols), dtype, x.device, "y")
-    mean = _out(mean, (rows,), torch.float32, x.device, "mean")
-    rstd = _out(rstd, (rows,), torch.float32, x.device, "rstd")
+    dtype, device = _rows_dtype(x), x.device
+    y = _out(y, (rows, cols), dtype, device, "y")
+    mean = _out(mean, (rows,), torch.float32, device, "mean")
+    rstd = _out(rstd, (rows,), torch.float32, device, "rstd")
     _on_current_device(x, gamma, beta, y, mean, rstd)
-    _check(lib.switchback_layer_norm(_dev(x, dtype, 2), _SB_DTYPE[dtype], _vec(gamma, cols, x.device, "gamma"),
-                                     _vec(beta, cols, x.device, "beta"), eps, rows, cols, _dev(y, dtype, 2),
+    _check(lib.switchback_layer_norm(_dev(x, dtype, 2), _SB_DTYPE[dtype], _vec(gamma, cols, device, "gamma"),
+                                     _vec(beta, cols, device, "beta"), eps, rows, cols, _dev(y, dtype, 2),
                                      _dev(mean, torch.float32), _dev(rstd, torch.float32), _stream()))
     return y, mean, rstd
 
@@ -841,23 +841,23 @@ def layer_norm_backward(dy, x, mean, rstd, gamma=None, affine=True, dx=None, dga
     affine=False)."""
     lib = _entries()
     rows, cols = x.shape
-    dtype = _rows_dtype(x)
-    _out(dy, (rows, cols), dtype, x.device, "dy")
-    _out(mean, (rows,), torch.float32, x.device, "mean")
-    _out(rstd, (rows,), torch.float32, x.device, "rstd")
-    dx = _out(dx, (rows, cols), dtype, x.device, "dx")
+    dtype, device = _rows_dtype(x), x.device
+    _out(dy, (rows, cols), dtype, device, "dy")
+    _out(mean, (rows,), torch.float32, device, "mean")
+    _out(rstd, (rows,), torch.float32, device, "rstd")
+    dx = _out(dx, (rows, cols), dtype, device, "dx")
     if affine:
-        dgamma = _out(dgamma, (cols,), torch.float32, x.device, "dgamma")
-        dbeta = _out(dbeta, (cols,), torch.float32, x.device, "dbeta")
+        dgamma = _out(dgamma, (cols,), torch.float32, device, "dgamma")
+        dbeta = _out(dbeta, (cols,), torch.float32, device, "dbeta")
         need = workspace_bytes(SB_OP_LAYER_NORM_BACKWARD, rows, cols, 0)  # none for few rows
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if ws is None and need else ws
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if ws is None and need else ws
     elif dgamma is not None or dbeta is not None:
         raise SwitchBackError("affine=False computes neither dgamma nor dbeta")
     _on_current_device(dy, x, mean, rstd, gamma, dx, dgamma, dbeta, ws)
     ws_at, ws_bytes = _given_ws(ws)
     _check(lib.switchback_layer_norm_backward(
         _dev(dy, dtype, 2), _dev(x, dtype, 2), _SB_DTYPE[dtype], _dev(mean, torch.float32), _dev(rstd, torch.float32),
-        _vec(gamma, cols, x.device, "gamma"), rows, cols, _dev(dx, dtype, 2), _dev(dgamma, torch.float32, 1) if affine else None,
+        _vec(gamma, cols, device, "gamma"), rows, cols, _dev(dx, dtype, 2), _dev(dgamma, torch.float32, 1) if affine else None,
         _dev(dbeta, torch.float32, 1) if affine else None, ws_at, ws_bytes, _stream()))
     return dx, dgamma, dbeta
 

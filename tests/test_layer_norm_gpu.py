@@ -89,7 +89,8 @@ def test_without_weights(n, dtype):
     check_backward(dy, x, mean.cpu(), rstd.cpu(), None, dx2, dgamma, dbeta)
 
 
-@pytest.mark.parametrize("b,n", [(512, 2056), (513, 2056), (512, 9000), (513, 9000), (511, 8200), (512, 1001), (514, 12001), (4099, 320), (20000, 72), (5000, 2304), (3000, 9000), (2500, 1003)])
+@pytest.mark.parametrize("b,n", [(512, 2056), (513, 2056), (512, 9000), (513, 9000), (511, 8200), (512, 1001), (514, 12001), (4099, 320), (20000, 72), (5000, 2304), (3000, 9000), (2500, 1003),
+                                 (2000, 5), (3000, 13), (5000, 67), (4000, 250), (2049, 12), (1500, 3001), (1100, 8191), (1300, 9001)])
 def test_many_rows(b, n):
     """More rows than groups that walk them: a group's registers carry sums from row to row."""
     x, dy, gamma, beta = rows_of(b, n, torch.bfloat16, b + n)
@@ -98,6 +99,14 @@ def test_many_rows(b, n):
     out = [sb.layer_norm_backward(on(dy), on(x), mean, rstd, on(gamma)) for _ in range(2)]
     check_backward(dy, x, mean.cpu(), rstd.cpu(), gamma, *out[0])
     assert all(torch.equal(p, q) for p, q in zip(*out)), "the same inputs give the same bits"
+
+
+@pytest.mark.parametrize("b,n", [(2000, 3), (3000, 13), (5000, 66), (4000, 250), (2049, 770), (1500, 3001), (1100, 8191), (1200, 4100)])
+def test_many_rows_in_f32(b, n):
+    x, dy, gamma, beta = rows_of(b, n, torch.float32, b + n)
+    y, mean, rstd = sb.layer_norm(on(x), on(gamma), on(beta))
+    check_forward(x, gamma, beta, 1e-5, y, mean, rstd)
+    check_backward(dy, x, mean.cpu(), rstd.cpu(), gamma, *sb.layer_norm_backward(on(dy), on(x), mean, rstd, on(gamma)))
 
 
 def test_no_rows():

@@ -4,7 +4,8 @@
 //   a = dy gamma,   dx = r (a - mean_j a - h mean_j(a h)),  dgamma_j = sum_i dy h,  dbeta_j = sum_i dy
 //
 // What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences from it
-// (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large).  Rows of up to 2048 columns belong to a
+// (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large), and the mean of these differences, by which
+the first one was off (2.5 % of the forward pass at 32896 x 1280 bf16, nothing elsewhere).  Rows of up to 2048 columns belong to a
 // wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and
 // beta (or its shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read
 // from L2 again.  Arithmetic is binary32; y and dx are rounded once.
@@ -121,6 +122,13 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*shared)[2][16]
     }
 }
 
+// The first mean is off by its sum's roundings, which a row far from zero multiplies by r (1920 columns of 10000: mean 10000.001, y
+// -0.3).  The differences d from it are exact there, so their own mean is what it is off by, and the variance is that of d.
+__device__ __forceinline__ float reciprocal_deviation(float mean_of_squares, float off, float eps) {
+    const float var = mean_of_squares - off * off;
+    return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);  // NaN stays
+}
+
 // Rows of up to LANES * V * P columns; P pieces a lane.  mean and rstd may be null, and gamma and beta.
 template <class T, int V, int P, int LANES, bool WHOLE>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
@@ -168,22 +176,23 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
             }
         if (row + step < rows) request(row + step);
         group_sums<LANES, 1>(s, shared, 0);
-        const float mu = s[0] * inv;
-        s[0] = 0.0f;
+        const float near = s[0] * inv;
+        float t[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             const bool in = (lane + p * G::LANES) * V < cols;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                v[p][e] = in ? v[p][e] - mu : 0.0f;
+                v[p][e] = in ? v[p][e] - near : 0.0f;
                 const float d = WHOLE || e >= shared_with[p] ? v[p][e] : 0.0f;
-                s[0] = fmaf(d, d, s[0]);
+                t[0] = fmaf(d, d, t[0]);
+                t[1] += d;
             }
         }
-        group_sums<LANES, 1>(s, shared, 1);
-        const float r = 1.0f / sqrtf(s[0] * inv + eps);
+        group_sums<LANES, 2>(t, shared, 1);
+        const float off = t[1] * inv, r = reciprocal_deviation(t[0] * inv, off, eps);
         if (lane == 0) {
-            if (mean != nullptr) mean[row] = mu;
+            if (mean != nullptr) mean[row] = near + off;
             if (rstd != nullptr) rstd[row] = r;
         }
 #pragma unroll
@@ -191,7 +200,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
             const int c = (lane + p * G::LANES) * V;
             float out[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = fmaf(v[p][e] * r, g[p][e], b[p][e]);
+            for (int e = 0; e < V; ++e) out[e] = fmaf((v[p][e] - off) * r, g[p][e], b[p][e]);
             if (c < cols) store_piece<T, V, WHOLE>(y + row * cols + at[p], out);
         }
     }
@@ -215,21 +224,22 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
             for (int e = 0; e < V; ++e) s[0] += at + e >= c ? widen(q.e[e]) : 0.0f;
         }
         group_sums<1024, 1>(s, shared, 0);
-        const float mu = s[0] * inv;
-        s[0] = 0.0f;
+        const float near = s[0] * inv;
+        float t[2] = {0.0f, 0.0f};
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
             const int at = piece_at<V, WHOLE>(c, cols);
             const Piece<T, V> q = load_piece<T, V, WHOLE, false>(xr + at);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = at + e >= c ? widen(q.e[e]) - mu : 0.0f;
-                s[0] = fmaf(d, d, s[0]);
+                const float d = at + e >= c ? widen(q.e[e]) - near : 0.0f;
+                t[0] = fmaf(d, d, t[0]);
+                t[1] += d;
             }
         }
-        group_sums<1024, 1>(s, shared, 1);
-        const float r = 1.0f / sqrtf(s[0] * inv + eps);
+        group_sums<1024, 2>(t, shared, 1);
+        const float off = t[1] * inv, r = reciprocal_deviation(t[0] * inv, off, eps);
         if (threadIdx.x == 0) {
-            if (mean != nullptr) mean[row] = mu;
+            if (mean != nullptr) mean[row] = near + off;
             if (rstd != nullptr) rstd[row] = r;
         }
         for (int c = threadIdx.x * V; c < cols; c += 1024 * V) {
@@ -241,7 +251,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restri
             if (gamma != nullptr) load_vector<V, WHOLE>(gamma, at, g);
             if (beta != nullptr) load_vector<V, WHOLE>(beta, at, b);
 #pragma unroll
-            for (int e = 0; e < V; ++e) out[e] = fmaf((widen(q.e[e]) - mu) * r, g[e], b[e]);
+            for (int e = 0; e < V; ++e) out[e] = fmaf((widen(q.e[e]) - near - off) * r, g[e], b[e]);
             store_piece<T, V, WHOLE>(y + row * cols + at, out);
         }
     }

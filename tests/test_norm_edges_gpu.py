@@ -1,0 +1,38 @@
+"""Layer norm at the edges of what it allows, on the GPU."""
+import pytest
+import torch
+
+import block_reference as ref
+from paper_2304_13013_amd import switchback as sb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPE = pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+
+
+@TYPE
+@pytest.mark.parametrize("n", [100, 640, 1088, 1280, 1920, 2047, 4100, 8191, 8193, 12296, 16388, 30000, 65535])
+def test_norm_of_rows_far_from_zero(n, dtype):
+    """Constant rows give zeros, and rows of a few steps around a large value what these steps give.
+
+    Tolerances.  A first mean is off by at most C |mu| (C = 128 * 2^-24, sums over lanes and waves).  Differences from it are exact
+    (both lie within a factor of two), of size S + C |mu| with S the row's largest distance from its mean, and their mean c is off
+    by C times that; so are the differences less c, and y by r times it.  The variance is the mean of their squares less c^2,
+    off by 4 C (S + C |mu|)^2."""
+    C = 128 * 2.0 ** -24
+    gen = torch.Generator().manual_seed(n)
+    x = torch.empty(7, n)
+    for i, value in enumerate((1000.0, 10000.0, 777.77, -1e5)):
+        x[i] = value
+    for i, value in enumerate((1000.0, 10000.0, -777.0)):
+        x[4 + i] = value + (8.0 if dtype == torch.bfloat16 else 2.0 ** -9) * torch.randint(-3, 4, (n,), generator=gen)
+    x = x.to(dtype)
+    y, mean, rstd = (t.cpu().double() for t in sb.layer_norm(x.to(DEV), eps=1e-5))
+    want, mu, r = ref.layer_norm(x, None, None, 1e-5)
+    size = (x.double() - mu[:, None]).abs().amax(1) + C * mu.abs()
+    assert ((mean - mu).abs() <= 2.0 ** -24 * mu.abs() + 2 * C * size).all(), "mean"
+    tol_r = C + 4 * C * size ** 2 * r ** 2
+    assert ((rstd - r).abs() <= tol_r * r).all(), "rstd"
+    tol = 2 * C * (size * r)[:, None] + want.abs() * tol_r[:, None]
+    off = (y - want).abs()
+    assert (off <= tol + torch.finfo(dtype).eps / 2 * (want.abs() + tol)).all(), "y off by %g" % float(off.max())

@@ -5,7 +5,7 @@
 //
 // What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences from it
 // (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large), and the mean of these differences, by which
-the first one was off (2.5 % of the forward pass at 32896 x 1280 bf16, nothing elsewhere).  Rows of up to 2048 columns belong to a
+// the first one was off (2.5 % of the forward pass at 32896 x 1280 bf16, nothing elsewhere).  Rows of up to 2048 columns belong to a
 // wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and
 // beta (or its shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read
 // from L2 again.  Arithmetic is binary32; y and dx are rounded once.

@@ -37,12 +37,15 @@ struct Piece {
 };
 typedef unsigned int v4u_at2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int v4u_at4 __attribute__((ext_vector_type(4), aligned(4)));
+// (Each type by its name: deduced as a template's argument it would lose its alignment.)
 template <int ALIGN, bool ONCE>
 __device__ __forceinline__ v4u load_quad(const void *at) {
-    auto load = [](auto *from) -> v4u { return ONCE ? __builtin_nontemporal_load(from) : *from; };
-    if constexpr (ALIGN == 2) return load(static_cast<const v4u_at2 *>(at));
-    else if constexpr (ALIGN == 4) return load(static_cast<const v4u_at4 *>(at));
-    else return load(static_cast<const v4u *>(at));
+    const v4u_at2 *at2 = static_cast<const v4u_at2 *>(at);
+    const v4u_at4 *at4 = static_cast<const v4u_at4 *>(at);
+    const v4u *at16 = static_cast<const v4u *>(at);
+    if constexpr (ALIGN == 2) return ONCE ? __builtin_nontemporal_load(at2) : *at2;
+    else if constexpr (ALIGN == 4) return ONCE ? __builtin_nontemporal_load(at4) : *at4;
+    else return ONCE ? __builtin_nontemporal_load(at16) : *at16;
 }
 template <int ALIGN>
 __device__ __forceinline__ void store_quad(void *at, v4u v) {

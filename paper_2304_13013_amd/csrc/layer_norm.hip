@@ -531,7 +531,7 @@ __global__ __launch_bounds__(1024) void layer_norm_reduce_kernel(const float *__
     }
 }
 
-constexpr int kLongParts = 256;  // shares of the rows where their sums are a launch of their own
+constexpr int kLongParts = 256;  // shares of the rows where their sums are a launch of their own, at most
 
 // Workgroups per compute unit that walk the rows: enough loads in flight, few partial sums.
 int walkers(int64_t rows, int per_block, int per_cu) {
@@ -605,7 +605,7 @@ bool sums_in_one_launch(int64_t rows, int cols, bool whole) {
 // four rows at least (600 x 16384: 41.2 on 128 workgroups, 47.5 on 256); two for shorter ones unless that leaves a group fewer
 // than two rows (32896 x 1280: 50.4, 55.0 with one; 2500 x 2048 f32 27.6 / 21.4).
 int backward_blocks(int64_t rows, int cols, bool whole) {
-    if (cols > longest_row(whole)) return kLongParts;
+    if (cols > longest_row(whole)) return (int)(rows < kLongParts ? rows : kLongParts);
     if (cols > 2048) {
         const int64_t four = (rows + 3) / 4;
         return (int)(four < num_compute_units() ? four : num_compute_units());
@@ -635,7 +635,7 @@ hipError_t backward_of(const T *dy, const T *x, const float *mean, const float *
         if (!fits) {
             layer_norm_backward_long_kernel<T, V, WHOLE><<<walkers(rows, 1, 2), 1024, 0, stream>>>(dy, x, mean, rstd, gamma, rows, cols, dx);
             if (sums)
-                layer_norm_column_sums_kernel<T><<<dim3((cols + 255) / 256, kLongParts), 256, 0, stream>>>(dy, x, mean, rstd, rows,
+                layer_norm_column_sums_kernel<T><<<dim3((cols + 255) / 256, blocks), 256, 0, stream>>>(dy, x, mean, rstd, rows,
                                                                                                           cols, partial);
         }
         const hipError_t e = hipGetLastError();
@@ -652,7 +652,7 @@ size_t layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows <= 0) return 0;
     // Either type: rows of whole pieces of four elements need not be of whole pieces of eight.
     const int a = sums_in_one_launch(rows, (int)cols, true) ? 0 : backward_blocks(rows, (int)cols, true);
-    const int b = sums_in_one_launch(rows, (int)cols, false) ? 0 : backward_blocks(rows, (int)cols, false);
+    const int b = cols % 8 == 0 ? 0 : sums_in_one_launch(rows, (int)cols, false) ? 0 : backward_blocks(rows, (int)cols, false);
     return (size_t)(a > b ? a : b) * 2 * (size_t)cols * sizeof(float);
 }
 

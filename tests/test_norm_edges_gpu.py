@@ -36,3 +36,19 @@ def test_norm_of_rows_far_from_zero(n, dtype):
     tol = 2 * C * (size * r)[:, None] + want.abs() * tol_r[:, None]
     off = (y - want).abs()
     assert (off <= tol + torch.finfo(dtype).eps / 2 * (want.abs() + tol)).all(), "y off by %g" % float(off.max())
+
+
+@TYPE
+@pytest.mark.parametrize("b,n", [(4, 12288), (1, 16384), (64, 9000), (3, 16392), (4, 65536), (300, 16388)])
+def test_norm_gradients_in_the_workspace_asked_for(b, n, dtype):
+    """No more than the call asks for, and none where it asks for none."""
+    gen = torch.Generator().manual_seed(b + n)
+    x, dy = (torch.randn(b, n, generator=gen).to(dtype) for _ in range(2))
+    need = sb.workspace_bytes(sb.SB_OP_LAYER_NORM_BACKWARD, b, n, 0)
+    mean, rstd = torch.zeros(b, device=DEV), torch.ones(b, device=DEV)
+    store = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV)
+    dx, dgamma, dbeta = sb.layer_norm_backward(dy.to(DEV), x.to(DEV), mean, rstd, ws=store[:need] if need else None)
+    assert (store[need:] == 77).all()
+    want = ref.layer_norm_backward(dy, x, mean.cpu(), rstd.cpu(), None)
+    for got, wide, size in ((dgamma, want[1], (dy.double() * x.double()).abs().sum(0)), (dbeta, want[2], dy.double().abs().sum(0))):
+        assert ((got.cpu().double() - wide).abs() <= (b / 256 + 128) * 2.0 ** -24 * size).all()

@@ -289,8 +289,9 @@ size_t switchback_backward_weight_experts_workspace_bytes(int64_t b, int64_t n, 
  *   dy, dx [rows,cols] in dtype; mean, rstd as the forward pass left them; gamma [cols] f32 or NULL; dgamma, dbeta [cols] f32,
  *   either or both NULL; their sums are formed in a fixed order (deterministic; no rows give zeros).
  *   ws: SB_OP_LAYER_NORM_BACKWARD workspace (0 bytes for few rows; not needed if dgamma and dbeta are NULL).
- * 1 <= cols <= 65536, rows <= 2^30; matrices, gamma and beta 16-byte aligned (dgamma, dbeta, mean, rstd 4-byte).  Outputs and
- * the workspace overlap neither each other nor the inputs: y = x and dx = dy are refused. */
+ * 1 <= cols <= 65536, rows <= 2^30; gamma, beta and matrices whose rows are multiples of 16 bytes are 16-byte aligned, other
+ * matrices like their elements; dgamma, dbeta, mean, rstd 4-byte.  Outputs and the workspace overlap neither each other nor the
+ * inputs: y = x and dx = dy are refused. */
 int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, const float *beta, float eps, int64_t rows,
                           int64_t cols, void *y, float *mean, float *rstd, void *stream);
 int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype, const float *mean, const float *rstd,

@@ -1,4 +1,4 @@
-"""Layer norm at the edges of what it allows, on the GPU."""
+"""Layer norm at the edges of what it allows, on the GPU: rows far from zero, rows that start anywhere, the widest rows."""
 import pytest
 import torch
 
@@ -52,3 +52,19 @@ def test_norm_gradients_in_the_workspace_asked_for(b, n, dtype):
     want = ref.layer_norm_backward(dy, x, mean.cpu(), rstd.cpu(), None)
     for got, wide, size in ((dgamma, want[1], (dy.double() * x.double()).abs().sum(0)), (dbeta, want[2], dy.double().abs().sum(0))):
         assert ((got.cpu().double() - wide).abs() <= (b / 256 + 128) * 2.0 ** -24 * size).all()
+
+
+@TYPE
+@pytest.mark.parametrize("b,n", [(6, 3), (6, 7), (9, 13), (40, 1001), (5, 8191), (4, 8193), (1500, 67)])
+def test_norm_of_rows_that_start_anywhere(b, n, dtype):
+    """Rows that are no whole 16-byte pieces need not start at one: views from the second row on, and outputs in such views."""
+    gen = torch.Generator().manual_seed(b + n)
+    x, dy = (torch.randn(b + 1, n, generator=gen).to(dtype).to(DEV) for _ in range(2))
+    gamma, beta = torch.rand(n, generator=gen).to(DEV), torch.rand(n, generator=gen).to(DEV)
+    want = sb.layer_norm(x[1:].clone(), gamma, beta)
+    y, dx = torch.full_like(x, -3.0), torch.full_like(x, -3.0)
+    got = sb.layer_norm(x[1:], gamma, beta, y=y[1:])
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and (y[0] == -3.0).all()
+    back = sb.layer_norm_backward(dy[1:].clone(), x[1:].clone(), want[1], want[2], gamma)
+    got = sb.layer_norm_backward(dy[1:], x[1:], want[1], want[2], gamma, dx=dx[1:])
+    assert all(torch.equal(p, q) for p, q in zip(got, back)) and (dx[0] == -3.0).all()

@@ -1,5 +1,14 @@
-"""Layer norm's workspace on the host: what its gradients ask for, and no more."""
+"""Layer norm's workspace and alignment on the host: what its calls ask for, and no more."""
+import ctypes
+
+import pytest
+
 from paper_2304_13013_amd import switchback as sb
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return sb.load_library()
 
 
 def test_workspace_of_wide_rows():
@@ -10,3 +19,15 @@ def test_workspace_of_wide_rows():
     assert need(4, 8193) == 4 * 2 * 8193 * 4 and need(4, 9004) == 4 * 2 * 9004 * 4
     assert need(3, 16392) == 3 * 2 * 16392 * 4 and need(1, 65536) == 2 * 65536 * 4
     assert need(256, 20000) == need(100000, 20000) == 256 * 2 * 20000 * 4
+
+
+def test_rows_start_at_an_element(lib):
+    at = ctypes.c_void_p  # never dereferenced
+    good, null = at(0x1000), at(None)
+    norm = lambda x, y, dtype, cols: lib.switchback_layer_norm(x, dtype, null, null, 1e-5, 4, cols, y, null, null, null)
+    back = lambda dy, x, dx, dtype, cols: lib.switchback_layer_norm_backward(dy, x, dtype, good, good, null, 4, cols, dx, null, null, null, 0, null)
+    for dtype, odd in ((0, 0x100001), (1, 0x100002)):
+        assert norm(at(odd), good, dtype, 63) == norm(good, at(odd), dtype, 63) == 1
+        assert back(at(odd), good, good, dtype, 63) == back(good, at(odd), good, dtype, 63) == back(good, good, at(odd), dtype, 63) == 1
+    for dtype, cols in ((0, 64), (1, 60)):
+        assert norm(at(0x100008), good, dtype, cols) == back(good, at(0x100008), good, dtype, cols) == 1

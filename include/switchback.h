@@ -228,7 +228,9 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  *   e = the least integer >= -127 with absmax(block) <= MAX * 2^e   (MAX = 448 for SB_E4M3, 57344 for SB_E5M2),
  *   code = float8cast(x * 2^-e), round to nearest even;   scale byte = e + 127;   the block stands for value(code) * 2^e,
  * so that nothing but the cast rounds, and Q(W^T) = Q(W)^T with the same scales.  A block without a nonzero value has scale
- * byte 0.  Scale bytes are 0 .. 247.
+ * byte 0.  Scale bytes are 0 .. 247.  A block with an infinity or a NaN has scale byte 247 (SB_E4M3) or 240 or 241 (SB_E5M2) and
+ * codes there that are not finite, its other values are cast with that scale, most of them to zero; so are, of a product, the
+ * outputs that such a code enters not finite, and all others those of the codes as they are.
  *
  * Layouts.  Code rows are whole blocks: K = the row's length rounded up to a multiple of 128, zero codes behind its end.
  * Row scales: [S, rows, 4] bytes with S = ceil(K / 512): byte q of row i in part s belongs to block 4 s + q of the row, 0 behind

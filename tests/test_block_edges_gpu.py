@@ -1,0 +1,71 @@
+"""The block-scaled float8 layer at the edges of what it allows, on the GPU."""
+import pytest
+import torch
+
+import block_reference as ref
+from paper_2304_13013_amd import switchback as sb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+E4M3, E5M2 = sb.SB_E4M3, sb.SB_E5M2
+FMT = pytest.mark.parametrize("fmt", [E4M3, E5M2], ids=["e4m3", "e5m2"])
+
+
+@FMT
+def test_blocks_with_values_that_are_not_finite(fmt):
+    """Infinities and every kind of NaN: their codes are not finite, their block has a documented scale, the other blocks are
+    those of the same rows without them."""
+    gen = torch.Generator().manual_seed(7)
+    x = torch.randn(40, 576, generator=gen).bfloat16()
+    bits = {(3, 5): 0x7f80, (9, 130): 0x7fc0, (12, 517): 0x7fff, (20, 300): -0x80, (20, 301): -1, (33, 0): 0x7fe1, (39, 575): 0x7f81}
+    clean = x.clone()
+    for (i, j), pattern in bits.items():
+        x[i, j:j + 1] = torch.tensor([pattern], dtype=torch.int16).view(torch.bfloat16)
+        clean[i, j // 128 * 128:(j // 128 + 1) * 128] = 0.0
+    codes, scales = (t.cpu() for t in sb.quantize_rowwise_f8_block(x.to(DEV), fmt))
+    want, e = ref.quantize_rows(clean, fmt)
+    values = ref.decode(codes, fmt)
+    exponents = scales.transpose(0, 1).reshape(40, -1)[:, :5].long() - 127
+    bad = {(i, j // 128) for i, j in bits}
+    for i in range(40):
+        for block in range(5):
+            at = slice(block * 128, (block + 1) * 128)
+            if (i, block) not in bad:
+                assert torch.equal(values[i, at], want[i, at]) and exponents[i, block] == e[i, block]
+                continue
+            assert (240 if fmt == E5M2 else 247) <= exponents[i, block] + 127 <= 247
+            for j in range(block * 128, min((block + 1) * 128, 576)):
+                if (i, j) in bits:
+                    assert not torch.isfinite(values[i, j])
+                else:
+                    assert values[i, j] == ref.to_format(x[i, j].double() / ref.power(exponents[i, block]), fmt)
+    # The product: rows with such values are not finite, the others what they are without them, by the quantizer and the product
+    # and by the kernel that quantizes a few rows itself.
+    w = torch.randn(192, 576, generator=gen).bfloat16()
+    wq, sw, _, _ = sb.quantize_weight_f8_block(w.to(DEV), E4M3)
+    rows = sorted({i for i, _ in bits})
+    others = [i for i in range(40) if i not in rows]
+    linear = [sb.linear_f8_block(t.to(DEV), wq, sw, fmt_x=fmt, y_dtype=torch.float32).cpu() for t in (x, clean)]
+    product = [sb.matmul_f8_block(*(lambda c, s: (c, fmt, s))(*sb.quantize_rowwise_f8_block(t.to(DEV), fmt)), wq, E4M3, sw,
+                                  out_dtype=torch.float32).cpu() for t in (x, clean)]
+    for given, without in (linear, product):
+        assert torch.equal(given[others], without[others]) and torch.isfinite(without).all() and not torch.isfinite(given[rows]).any()
+
+
+@FMT
+def test_weight_blocks_with_values_that_are_not_finite(fmt):
+    gen = torch.Generator().manual_seed(8)
+    x, w = torch.randn(300, 320, generator=gen).bfloat16(), torch.randn(2, 320, 320, generator=gen).bfloat16()
+    clean = w.clone()
+    w[1, 200, 70:71] = torch.tensor([0x7fff], dtype=torch.int16).view(torch.bfloat16)
+    out, want = (sb.quantize_weight_f8_block(t.to(DEV), fmt) for t in (w, clean))
+    scales = out[1].cpu()
+    assert scales[1, 1, 0] == (247 if fmt == E4M3 else 241) and out[3].cpu()[1, 0, 1] == scales[1, 1, 0]
+    scales[1, 1, 0] = want[1].cpu()[1, 1, 0]
+    assert torch.equal(scales, want[1].cpu())
+    where = torch.tensor([0, 100, 300], dtype=torch.int32, device=DEV)
+    y, without = (sb.linear_f8_block(x.to(DEV), c, s, offsets=where, fmt_w=fmt, y_dtype=torch.float32).cpu() for c, s, _, _ in (out, want))
+    assert not torch.isfinite(y[100:, 200]).any() and torch.equal(y[:100], without[:100])
+    others = list(range(128)) + list(range(256, 320))
+    assert torch.equal(y[100:][:, others], without[100:][:, others])
+    assert torch.isfinite(y[100:, [j for j in range(128, 256) if j != 200]]).all()

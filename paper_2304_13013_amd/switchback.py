@@ -591,7 +591,9 @@ def backward_input_f8(dy, bufs, dx=None, dx_dtype=torch.bfloat16, fmt_g=SB_E5M2,
 # ---- float8 with a scale for each block of 128, plain or with a weight per expert -----------------------------------
 # Codes are uint8 tensors with rows of whole blocks (zeros behind the row's end), scales uint8 exponents e + 127: a block
 # stands for value(code) * 2^e.  Weights of experts are [experts, m, n] and go with `offsets`, int32 [experts + 1] on the GPU:
-# rows offsets[e] .. offsets[e + 1] - 1 are expert e's, rows past the last offset no one's, whose outputs stay as they were.
+# rows offsets[e] .. offsets[e + 1] - 1 are expert e's; rows before the first offset and past the last one are no one's: they stay as
+# they were in an output that the caller gives, and are zero in one that the call makes (where they fall is known on the GPU alone,
+# so that is all of it cleared first: a loop keeps its outputs).
 
 def _on_current_device(*tensors):
     """The calls below enqueue on the current device's stream: their tensors have to be there (those on no GPU at all are refused
@@ -605,6 +607,13 @@ def _on_current_device(*tensors):
 def _given_ws(ws):
     """Address and bytes of a workspace, or of none."""
     return (None, 0) if ws is None else (_dev(ws, ws.dtype), ws.numel() * ws.element_size())
+
+
+def _rows_out(t, shape, dtype, device, name, offsets):
+    """An output of rows that the kernels may leave out, if they go by experts."""
+    if t is None and offsets is not None:
+        return torch.zeros(shape, dtype=dtype, device=device)
+    return _out(t, shape, dtype, device, name)
 
 
 def _whole_blocks(cols):
@@ -685,7 +694,7 @@ def matmul_f8_block(aq, fmt_a, scales_a, bq, fmt_b, scales_b, offsets=None, out=
     out_dtype = out_dtype if out is None else out.dtype
     if out_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("out must be bf16 or f32")
-    out = _out(out, (M, N), out_dtype, aq.device, "out")
+    out = _rows_out(out, (M, N), out_dtype, aq.device, "out", offsets)
     _out(scales_a, _row_scales(M, K), torch.uint8, aq.device, "scales_a")
     _on_current_device(aq, scales_a, bq, scales_b, offsets, out)
     _check(lib.switchback_matmul_f8_block(
@@ -706,7 +715,7 @@ def linear_f8_block(x, wq, scales_w, offsets=None, fmt_x=SB_E4M3, fmt_w=SB_E4M3,
     y_dtype = y_dtype if y is None else y.dtype
     if y_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("y must be bf16 or f32")
-    y = _out(y, (b, m), y_dtype, x.device, "y")
+    y = _rows_out(y, (b, m), y_dtype, x.device, "y", offsets)
     if ws is None:
         need = lib.switchback_linear_f8_block_workspace_bytes(b, n, m, experts)  # none for few rows
         ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
@@ -756,7 +765,7 @@ def forward_f8_block(x, w, bufs=None, offsets=None, y=None, y_dtype=torch.bfloat
     y_dtype = y_dtype if y is None else y.dtype
     if y_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("y must be bf16 or f32")
-    y = _out(y, (b, m), y_dtype, x.device, "y")
+    y = _rows_out(y, (b, m), y_dtype, x.device, "y", offsets)
     _on_current_device(x, w, offsets, y, bufs.wq)
     _check(lib.switchback_forward_f8_block(
         _dev(x, torch.bfloat16, 2), _dev(w, torch.bfloat16), where, experts, b, n, m, fmt_x, fmt_w, _dev(bufs.wq, torch.uint8),
@@ -775,7 +784,7 @@ def backward_input_f8_block(dy, bufs, offsets=None, dx=None, dx_dtype=torch.bflo
     dx_dtype = dx_dtype if dx is None else dx.dtype
     if dx_dtype not in (torch.bfloat16, torch.float32):
         raise SwitchBackError("dx must be bf16 or f32")
-    dx = _out(dx, (b, bufs.n), dx_dtype, dy.device, "dx")
+    dx = _rows_out(dx, (b, bufs.n), dx_dtype, dy.device, "dx", offsets)
     _on_current_device(dy, offsets, dx, bufs.wq)
     _check(lib.switchback_linear_f8_block(
         _dev(dy, torch.bfloat16, 2), _dev(bufs.wq_t, torch.uint8), _dev(bufs.scales_wt, torch.uint8), where, bufs.experts or 1, b, m,

@@ -69,3 +69,30 @@ def test_weight_blocks_with_values_that_are_not_finite(fmt):
     others = list(range(128)) + list(range(256, 320))
     assert torch.equal(y[100:][:, others], without[100:][:, others])
     assert torch.isfinite(y[100:, [j for j in range(128, 256) if j != 200]]).all()
+
+
+@pytest.mark.parametrize("b", [3, 40, 700], ids=["few", "blocks", "more"])
+def test_rows_of_no_expert_in_outputs_of_the_call(b):
+    """Outputs that the call makes hold zeros there, so that what reads all rows (a norm's gradient) reads no garbage."""
+    n, m, experts = 192, 320, 3
+    gen = torch.Generator().manual_seed(b)
+    x, dy, w = (torch.randn(*s, generator=gen).bfloat16().to(DEV) for s in ((b, n), (b, m), (experts, m, n)))
+    where = torch.tensor([1, 1, 2, b // 2 + 1], dtype=torch.int32, device=DEV)
+    rest = [0] + list(range(b // 2 + 1, b))
+
+    def garbage(width, dtype):  # what the allocator hands out next
+        for _ in range(2):
+            torch.full((b, width), float("nan"), dtype=dtype, device=DEV)
+
+    for dtype in (torch.bfloat16, torch.float32):
+        garbage(m, dtype)
+        y, bufs = sb.forward_f8_block(x, w, sb.BlockBuffers(b, n, m, experts), offsets=where, y_dtype=dtype)
+        garbage(n, dtype)
+        dx = sb.backward_input_f8_block(dy, bufs, offsets=where, dx_dtype=dtype)
+        garbage(m, dtype)
+        kept = sb.linear_f8_block(x, bufs.wq, bufs.scales_w, offsets=where, y_dtype=dtype)
+        codes, scales = sb.quantize_rowwise_f8_block(x, E4M3)
+        garbage(m, dtype)
+        out = sb.matmul_f8_block(codes, E4M3, scales, bufs.wq, E4M3, bufs.scales_w, offsets=where, out_dtype=dtype)
+        for t in (y, dx, kept, out):
+            assert not t[rest].any() and t[1:b // 2 + 1].any(1).all()

@@ -261,7 +261,8 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  *   NULL) and X, then the product.  ws: SB_OP_FORWARD_F8_BLOCK workspace.  b == 0 still quantizes W.  m % 64 == 0, n % 64 == 0;
  *   other limits as above.
  * The weight gradient of the plain layer is switchback_backward_weight, with experts switchback_backward_weight_experts: dW[e]
- *   = dY^T X over the rows of expert e, 16-bit operands, binary32 accumulation; zeros for an expert without rows.  dw
+ *   = dY^T X over the rows of expert e, 16-bit operands, binary32 accumulation (of many rows in pieces of about 4096, so that its
+ *   error does not grow with them); zeros for an expert without rows.  dw
  *   [experts,m,n], SB_BF16 or SB_F32; ws: switchback_backward_weight_experts_workspace_bytes(b, n, m, experts) bytes. */
 int switchback_quantize_rowwise_f8_block(const void *x_bf16, int64_t rows, int64_t cols, sb_f8_format fmt, uint8_t *codes,
                                          uint8_t *scales, void *stream);

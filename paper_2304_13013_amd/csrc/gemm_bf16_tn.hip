@@ -33,7 +33,7 @@ __global__ __launch_bounds__(Big::THREADS) __attribute__((amdgpu_waves_per_eu(1,
 }
 __global__ __launch_bounds__(Small::THREADS) __attribute__((amdgpu_waves_per_eu(2))) void gemm_bf16_tn_experts_small_kernel(
     GemmBf16ExpertArgs p) {
-    gemm_bf16_tn_body<false>(p);
+    gemm_bf16_tn_body<true>(p);
 }
 
 // out[e] = sum over splits (ascending) of partial[s][e]; four elements per thread, eight splits' loads in flight.
@@ -122,8 +122,28 @@ ExpertGradPlan plan_gemm_bf16_tn_experts(int64_t b, int64_t n, int64_t m, int64_
     return plan_expert_gradient(b, n, m, experts, num_compute_units());
 }
 
-size_t gemm_bf16_tn_experts_workspace_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts) {
+namespace {
+
+// Persistent, as above: an item's first stages are requested under the one before it, and in every round the XCDs work on
+// neighbouring tiles.  A workgroup per item instead balances experts of different lengths no better: 64 experts of 250
+// tokens, 2048 -> 2048 269 / 234 us so; 16 uneven ones, 30000 tokens, 2048 -> 1024 161 / 150; 8 uneven ones, 16448 tokens,
+// 1024 -> 4096 115 / 111 (of one length 103 / 109).
+int experts_grid(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts) {
+    const int side = plan.small ? 128 : 256;
+    const int64_t total = ((m + side - 1) / side) * ((n + side - 1) / side) * plan.splits * experts;
+    const int64_t per_xcd = (total + 7) / 8, slots_per_xcd = (num_compute_units() / 8 > 0 ? num_compute_units() / 8 : 1) * (plan.small ? 2 : 1);
+    return (int)(8 * (per_xcd < slots_per_xcd ? per_xcd : slots_per_xcd));
+}
+size_t experts_partial_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts) {
     return plan.splits > 1 ? (size_t)plan.splits * (size_t)experts * (size_t)m * (size_t)n * sizeof(float) : 0;
+}
+
+}  // namespace
+
+// The splits' partial sums, then a tile for each workgroup whose items may be summed in pieces.
+size_t gemm_bf16_tn_experts_workspace_bytes(const ExpertGradPlan &plan, int64_t n, int64_t m, int64_t experts) {
+    return experts_partial_bytes(plan, n, m, experts) +
+           (plan.pieces ? (size_t)experts_grid(plan, n, m, experts) * Big::BM * Big::BN * sizeof(float) : 0);
 }
 
 hipError_t launch_gemm_bf16_tn_experts(const ExpertGradPlan &plan, const void *dy, const void *x, const int32_t *offsets, int64_t experts,
@@ -148,13 +168,8 @@ hipError_t launch_gemm_bf16_tn_experts(const ExpertGradPlan &plan, const void *d
     a.out_bf16 = dw_dtype == SB_BF16;
     a.offsets = offsets;
     a.experts = (int)experts;
-    // Persistent, as above: an item's first stages are requested under the one before it, and in every round the XCDs work on
-    // neighbouring tiles.  A workgroup per item instead balances experts of different lengths no better: 64 experts of 250
-    // tokens, 2048 -> 2048 269 / 234 us so; 16 uneven ones, 30000 tokens, 2048 -> 1024 161 / 150; 8 uneven ones, 16448 tokens,
-    // 1024 -> 4096 115 / 111 (of one length 103 / 109).
-    const int64_t total = (int64_t)a.tiles_m * a.tiles_n * a.splits * experts;
-    const int64_t per_xcd = (total + 7) / 8, slots_per_xcd = (num_compute_units() / 8 > 0 ? num_compute_units() / 8 : 1) * (plan.small ? 2 : 1);
-    const int grid = (int)(8 * (per_xcd < slots_per_xcd ? per_xcd : slots_per_xcd));
+    a.pieces = reinterpret_cast<v4f *>(static_cast<char *>(ws) + experts_partial_bytes(plan, n, m, experts));
+    const int grid = experts_grid(plan, n, m, experts);
     if (plan.small)
         gemm_bf16_tn_experts_small_kernel<<<grid, Small::THREADS, Small::LDS_BYTES, stream>>>(a);
     else

@@ -41,6 +41,7 @@ struct GemmBf16Args {
 struct GemmBf16ExpertArgs : GemmBf16Args {
     const int *offsets;  // [experts + 1]
     int experts;
+    v4f *pieces;  // 256x256 tiles: a tile of binary32 for every workgroup, if an item may be summed in pieces (ExpertGradPlan)
 };
 
 // The tokens of one split of an expert's range, clamped to what there is; a split is whole stages of the range.
@@ -55,6 +56,12 @@ __device__ __forceinline__ ExpertTokens expert_tokens(const GemmBf16ExpertArgs &
     t.first = __builtin_amdgcn_readfirstlane(min(first + split * per, end));
     t.end = __builtin_amdgcn_readfirstlane(min(t.first + per, end));
     return t;
+}
+
+// Stages of a piece of an item's `stages`: an even share, of about DW_PIECE.
+__device__ __forceinline__ int piece_stages(int stages) {
+    const int pieces = max((stages + DW_PIECE / 2) / DW_PIECE, 1);
+    return (stages + pieces - 1) / pieces;
 }
 
 // 80 KiB of LDS, so two workgroups share a compute unit; all four waves load.
@@ -79,7 +86,7 @@ struct GemmBf16Cfg {
 
 // FOLD: the token range is one item, but its pieces of k_per_piece tokens are summed on their own and added in token
 // order, in registers: the bits of the split product and its reduction, without the second launch.
-// With GemmBf16ExpertArgs an expert without tokens gets zeros.
+// With GemmBf16ExpertArgs (FOLD, for the pieces of long items) an expert without tokens gets zeros.
 // (A __device__ function: a __global__ template that uses device-only buffer builtins does not instantiate in the host
 // pass; the __global__ entries live next to the launcher.)
 template <bool FOLD, class Args>
@@ -303,8 +310,10 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
             }
         };
         v16f pieces[FOLD ? MT : 1][FOLD ? C::NT : 1];  // sum of the pieces before this one
-        int piece_left = FOLD ? p.k_per_piece / C::BKT : 0;
-        if constexpr (FOLD) {
+        const int per_piece = EXPERTS ? piece_stages(KT) : FOLD ? p.k_per_piece / C::BKT : 0;
+        int piece_left = per_piece;
+        bool before = false;  // EXPERTS: whether there is a piece before this one
+        if constexpr (FOLD && !EXPERTS) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -314,16 +323,17 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
         }
         auto end_piece = [&]() {
             if constexpr (FOLD) {
-                piece_left = p.k_per_piece / C::BKT;
+                piece_left = per_piece;
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int nt = 0; nt < C::NT; ++nt)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
-                            pieces[mt][nt][r] += acc[mt][nt][r];
+                            pieces[mt][nt][r] = (EXPERTS && !before ? 0.0f : pieces[mt][nt][r]) + acc[mt][nt][r];
                             acc[mt][nt][r] = 0.0f;
                         }
+                before = true;
             }
         };
         if (KT > 0) {
@@ -336,7 +346,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
                 if (FOLD && --piece_left == 0) end_piece();
             }
             k_tile(KT - 1, std::true_type());
-            if constexpr (FOLD) {
+            if (FOLD && (!EXPERTS || before)) {
                 end_piece();
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)

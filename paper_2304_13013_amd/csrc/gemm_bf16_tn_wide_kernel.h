@@ -213,15 +213,74 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const Args &p) {
             advance();
             ++g;
         };
-        period(std::integral_constant<int, 0>(), std::true_type());
-        period(std::integral_constant<int, 1>(), std::false_type());
-        for (int kt = 2; kt < it.stages; kt += 2) {
-            period(std::integral_constant<int, 0>(), std::false_type());
+        // EXPERTS, an item of several pieces: the piece's sum and the sum of those before it, which waits in this workgroup's tile of
+        // the workspace (a lane's 16 bytes side by side), go back there, and the last one to the output.
+        auto end_piece = [&](bool before, bool last) __attribute__((always_inline)) {
+            constexpr unsigned TILE = C::BM * C::BN * 4, NOWHERE = 0x80000000u;
+            int lane_e = lane, n = p.n;  // opaque, as in the epilogue below
+            asm volatile("" : "+v"(lane_e));
+            asm volatile("" : "+s"(n));
+            const int m_base = it.tm * C::BM + wm0, n_base = it.tn * C::BN + wn0;
+            const unsigned rows_in = __builtin_amdgcn_readfirstlane(min(max(p.m - m_base, 0), C::WT));
+            v4f *tile = nullptr;
+            if constexpr (EXPERTS) tile = p.pieces + (int64_t)blockIdx.x * (TILE / 16);
+            const bool as_bf16 = last && p.splits == 1 && p.out_bf16;
+            const int bytes = as_bf16 ? 2 : 4;
+            char *out = reinterpret_cast<char *>(tile);
+            if constexpr (EXPERTS)
+                if (last)
+                    out = (p.splits > 1 ? reinterpret_cast<char *>(p.partial) : static_cast<char *>(p.out)) +
+                          (((int64_t)(p.splits > 1 ? it.split * p.experts + it.matrix : it.matrix) * p.m + m_base) * n + n_base) * bytes;
+            // The first piece finds nothing: zeros from the bounds check.
+            const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(tile, 0, before ? TILE : 0, 0x00020000);
+            const __amdgpu_buffer_rsrc_t to = __builtin_amdgcn_make_buffer_rsrc(out, 0, last ? rows_in * n * bytes : TILE, 0x00020000);
+            const unsigned mine = (unsigned)(wave * 64 + lane_e) * 16, voff = last ? (unsigned)((lane_e & 15) * n + (lane_e >> 4) * 4) * bytes : mine;
+            const unsigned row_step = last ? 16u * n * bytes : NB * C::THREADS * 16u, col_step = last ? 16u * bytes : C::THREADS * 16u;
+            const int cols_in = last ? p.n - n_base : C::WT;
+            wait_lds_reads();  // the next stage's fragments, which nobody may move before they are there
+            pin_frags(0);
+#pragma unroll
+            for (int a = 0; a < NB; ++a) {
+                v4f sum[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    sum[b] = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(from, mine, (a * NB + b) * (C::THREADS * 16), 0));
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float x;
+                        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[a][b][e]));
+                        sum[b][e] += x;
+                    }
+                    const unsigned to_col = b * 16 < cols_in ? voff : NOWHERE, step = a * row_step + b * col_step;
+                    if (as_bf16)
+                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2u, __builtin_convertvector(sum[b], v4bf)), to, to_col, step, 0);
+                    else
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, sum[b]), to, to_col, step, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const int per_piece = EXPERTS ? 2 * piece_stages(it.stages / 2) : it.stages;
+        for (int done = 0;;) {
+            const int stages = EXPERTS ? min(per_piece, it.stages - done) : it.stages;
+            period(std::integral_constant<int, 0>(), std::true_type());
             period(std::integral_constant<int, 1>(), std::false_type());
+            for (int kt = 2; kt < stages; kt += 2) {
+                period(std::integral_constant<int, 0>(), std::false_type());
+                period(std::integral_constant<int, 1>(), std::false_type());
+            }
+            // Nobody knows of the matrix instructions in the asm: their last results need up to 18 wait states.
+            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+            if constexpr (!EXPERTS) {
+                break;
+            } else {
+                done += stages;
+                if (per_piece < it.stages) end_piece(done > stages, done >= it.stages);
+                if (done >= it.stages) break;
+            }
         }
-        // Nobody knows of the matrix instructions in the asm: their last results need up to 18 wait states.
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-
         // A lane owns row l % 16 of dW and four consecutive columns of every block.  Rows past the end lie beyond the
         // buffer resource of the wave tile, columns past the end are sent there: the number of stores is always the same.
         const int m_base = it.tm * C::BM + wm0, n_base = it.tn * C::BN + wn0;
@@ -233,7 +292,9 @@ __device__ __forceinline__ void gemm_bf16_tn_wide_body(const Args &p) {
         asm volatile("" : "+s"(n));
         const int e_r = lane_e & 15, e_g = lane_e >> 4;
         constexpr unsigned NOWHERE = 0x80000000u;
-        if (p.splits == 1 && p.out_bf16) {
+        if (EXPERTS && per_piece < it.stages) {
+            // end_piece has stored it.
+        } else if (p.splits == 1 && p.out_bf16) {
             // Final bf16 result: transposed through the wave-private patch, 256-byte row segments.  Those of experts are
             // non-temporal: more than the L2s hold, next to operands that are read again (16000 tokens, 64 experts of 2048 x 2048:
             // 237 -> 157 us; 30000 tokens, 16 of 2048 x 1024 157 -> 152).

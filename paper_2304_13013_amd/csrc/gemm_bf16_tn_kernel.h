@@ -356,10 +356,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
         }
 
         const int m_base = tm * C::BM + wm0, n_base = tn * C::BN + wn0;
-        // Matrices before this item's in the output, or in the partial sums.
-        const int out_matrix = EXPERTS ? split / p.splits : 0;
-        int this_split = split;
-        if constexpr (EXPERTS) this_split = split % p.splits * p.experts + split / p.splits;
+        const int this_split = split;
 
         // Every wave is done reading the stages: request the next item's stages, then store this item's results.
         wait_lds_reads();
@@ -381,7 +378,8 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
             // them (rows past the end lie beyond the buffer resource, columns are sent there).  5003 tokens, 24 experts of 1088 x
             // 768, binary32, from memory: 50 us as below, 26 so; 1500 tokens 35.5 / 19.7.
             const bool as_bf16 = p.splits == 1 && p.out_bf16;
-            const int bytes = as_bf16 ? 2 : 4, matrix = p.splits > 1 ? this_split : out_matrix;
+            const int bytes = as_bf16 ? 2 : 4, expert = this_split / p.splits;
+            const int matrix = p.splits > 1 ? this_split % p.splits * p.experts + expert : expert;  // of the partial sums; of the output
             char *out = p.splits > 1 ? reinterpret_cast<char *>(p.partial) : static_cast<char *>(p.out);
             const unsigned rows_in = __builtin_amdgcn_readfirstlane(min(max(p.m - m_base, 0), C::WTM));
             const __amdgpu_buffer_rsrc_t rsrc_out = __builtin_amdgcn_make_buffer_rsrc(
@@ -418,7 +416,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
             stores_behind = as_bf16 ? MT * 4 / C::LPW : MT * C::NT * 4 / C::LPW;
         } else if (p.splits == 1 && p.out_bf16) {
             // Final bf16 result: transpose through the wave-private LDS patch, 16-byte stores in 128-byte row segments.
-            unsigned short *out = static_cast<unsigned short *>(p.out) + (EXPERTS ? (int64_t)out_matrix * p.m * p.n : 0);
+            unsigned short *out = static_cast<unsigned short *>(p.out);
             unsigned char *epi = smem + S * C::STAGE_BYTES + wave * C::EPI_WAVE_BYTES;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -445,8 +443,7 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
             }
         } else {
             // binary32: final result (one split) or this split's partial sums, straight from the registers.
-            float *pout = p.splits > 1 ? p.partial + (int64_t)this_split * p.m * p.n
-                                       : static_cast<float *>(p.out) + (EXPERTS ? (int64_t)out_matrix * p.m * p.n : 0);
+            float *pout = p.splits > 1 ? p.partial + (int64_t)this_split * p.m * p.n : static_cast<float *>(p.out);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll

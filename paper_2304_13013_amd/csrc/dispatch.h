@@ -383,7 +383,7 @@ enum { DW_PIECE = 64 };  // stages
 struct ExpertGradPlan {
     bool small;   // 128x128 tiles, else 256x256
     int splits;   // of every expert's tokens
-    bool pieces;  // 256x256 tiles: an item may have more than one, whose sum waits in the workspace
+    bool pieces;  // whether an item may have more than one: their sum waits in registers (128x128 tiles) or in the workspace
 };
 inline ExpertGradPlan plan_expert_gradient(int64_t b, int64_t n, int64_t m, int64_t experts, int ncu) {
     ExpertGradPlan plan{true, 1, false};
@@ -400,7 +400,7 @@ inline ExpertGradPlan plan_expert_gradient(int64_t b, int64_t n, int64_t m, int6
             }
         }
     }
-    plan.pieces = !plan.small && ((b + plan.splits - 1) / plan.splits + DW_STAGE - 1) / DW_STAGE >= DW_PIECE + DW_PIECE / 2;
+    plan.pieces = ((b + plan.splits - 1) / plan.splits + DW_STAGE - 1) / DW_STAGE >= DW_PIECE + DW_PIECE / 2;
     return plan;
 }
 

@@ -60,8 +60,8 @@ __device__ __forceinline__ ExpertTokens expert_tokens(const GemmBf16ExpertArgs &
 
 // Stages of a piece of an item's `stages`: an even share, of about DW_PIECE.
 __device__ __forceinline__ int piece_stages(int stages) {
-    const int pieces = max((stages + DW_PIECE / 2) / DW_PIECE, 1);
-    return (stages + pieces - 1) / pieces;
+    const int pieces = (stages + DW_PIECE / 2) / DW_PIECE;
+    return pieces <= 1 ? stages : (stages + pieces - 1) / pieces;
 }
 
 // 80 KiB of LDS, so two workgroups share a compute unit; all four waves load.

@@ -120,3 +120,23 @@ def test_typical_error_of_products(b, n, m, experts):
     xv = ref.row_values(*ref.quantize_rows(x, E4M3))[:, :n].to(DEV)
     want = torch.cat([xv[rows] @ values[e].t().contiguous() for e, rows in enumerate(ref.expert_slices(offsets or [0, b], b))])
     assert relative_error(y, want) <= 0.7 * 2.0 ** -13 and relative_error(served, want) <= 0.7 * 2.0 ** -13
+
+
+@pytest.mark.parametrize("b,n,m,experts", [(13, 320, 192, 5), (700, 1088, 576, 4)], ids=["few", "more"])
+def test_outputs_of_a_captured_call(b, n, m, experts):
+    """A graph that holds the call's own output: rows of no expert are zero in every replay, also where they had an expert before."""
+    gen = torch.Generator().manual_seed(b)
+    codes, scales, _, _ = sb.quantize_weight_f8_block(torch.randn(experts, m, n, generator=gen).bfloat16().to(DEV), E4M3)
+    x = torch.zeros(b, n, dtype=torch.bfloat16, device=DEV)
+    where = torch.zeros(experts + 1, dtype=torch.int32, device=DEV)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        y = sb.linear_f8_block(x, codes, scales, offsets=where)
+    for first, rest in ((0, 0), (2, 5), (0, 7), (4, 0), (1, 1)):
+        x.copy_(torch.randn(b, n, generator=gen).bfloat16())
+        where.copy_(torch.tensor([first + (b - first - rest) * e // experts for e in range(experts + 1)], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = sb.linear_f8_block(x, codes, scales, offsets=where, y=torch.zeros_like(y))
+        assert torch.equal(y, eager) and not y[:first].any() and not y[b - rest:].any()

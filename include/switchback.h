@@ -229,12 +229,13 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  *   code = float8cast(x * 2^-e), round to nearest even;   scale byte = e + 127;   the block stands for value(code) * 2^e,
  * so that nothing but the cast rounds, and Q(W^T) = Q(W)^T with the same scales.  A block without a nonzero value has scale
  * byte 0.  Scale bytes are 0 .. 247.  A block with an infinity or a NaN has scale byte 247 (SB_E4M3) or 240 or 241 (SB_E5M2) and
- * codes there that are not finite, its other values are cast with that scale, most of them to zero; so are, of a product, the
- * outputs that such a code enters not finite, and all others those of the codes as they are.
+ * codes there that are not finite; its other values are cast with that scale, most of them to zero.  Of a product, the outputs that
+ * such a code enters are not finite, the others are those of the codes as they are.
  *
  * Layouts.  Code rows are whole blocks: K = the row's length rounded up to a multiple of 128, zero codes behind its end.
  * Row scales: [S, rows, 4] bytes with S = ceil(K / 512): byte q of row i in part s belongs to block 4 s + q of the row, 0 behind
- * the last block.  Weight scales: [ceil(m / 128), K / 128] bytes.  All are 16-byte aligned.
+ * the last block.  Weight scales: [ceil(m / 128), K / 128] bytes, read four at a time: up to three bytes behind the last one, in
+ * its aligned four, have to be there (any allocation's are).  All are 16-byte aligned.
  *
  * Experts.  With offsets == NULL there is one weight (experts == 1) and it goes with all rows.  Otherwise weights, codes,
  * scales and weight gradients are [experts, ...] and `offsets` is a device array of experts + 1 non-decreasing int32 row
@@ -262,8 +263,8 @@ int switchback_backward_input_f8(const void *dy_bf16, const sb_saved *saved, int
  *   other limits as above.
  * The weight gradient of the plain layer is switchback_backward_weight, with experts switchback_backward_weight_experts: dW[e]
  *   = dY^T X over the rows of expert e, 16-bit operands, binary32 accumulation (of many rows in pieces of about 4096, so that its
- *   error does not grow with them); zeros for an expert without rows.  dw
- *   [experts,m,n], SB_BF16 or SB_F32; ws: switchback_backward_weight_experts_workspace_bytes(b, n, m, experts) bytes. */
+ *   error does not grow with them); zeros for an expert without rows.  dw [experts,m,n], SB_BF16 or SB_F32; ws:
+ *   switchback_backward_weight_experts_workspace_bytes(b, n, m, experts) bytes. */
 int switchback_quantize_rowwise_f8_block(const void *x_bf16, int64_t rows, int64_t cols, sb_f8_format fmt, uint8_t *codes,
                                          uint8_t *scales, void *stream);
 int switchback_quantize_weight_f8_block(const void *w_bf16, int64_t experts, int64_t m, int64_t n, sb_f8_format fmt,
@@ -286,7 +287,8 @@ size_t switchback_backward_weight_experts_workspace_bytes(int64_t b, int64_t n, 
 
 /* Layer norm over the rows of x [rows,cols] (SB_BF16 or SB_F32, `dtype`), the operation in front of a transformer block's
  * linear layers, with its gradients.  mu and r = 1 / sqrt(var + eps) per row (var the mean of the squared differences from
- * mu), h = (x - mu) * r, y = h * gamma + beta; binary32 arithmetic, y rounded once.
+ * mu), h = (x - mu) * r, y = h * gamma + beta; binary32 arithmetic, y rounded once.  The sum of (x - mu)^2 has to fit:
+ * |x - mu| < 1.8e19 / sqrt(cols).
  *   y [rows,cols] in dtype; gamma, beta [cols] f32 or NULL (1 and 0); mean, rstd [rows] f32 or NULL; eps > 0.
  * Backward, with a = dy * gamma:  dx = r * (a - mean_j(a) - h * mean_j(a * h)),  dgamma = sum_i dy * h,  dbeta = sum_i dy.
  *   dy, dx [rows,cols] in dtype; mean, rstd as the forward pass left them; gamma [cols] f32 or NULL; dgamma, dbeta [cols] f32,

@@ -376,7 +376,8 @@ __device__ __forceinline__ void gemm_bf16_tn_body(const Args &p) {
             // An expert's tokens are few stages and the gradients most of the traffic: whole 128-byte row segments through the
             // wave-private patch, non-temporal, and always the same number of stores, so that the next item's waits need not drain
             // them (rows past the end lie beyond the buffer resource, columns are sent there).  5003 tokens, 24 experts of 1088 x
-            // 768, binary32, from memory: 50 us as below, 26 so; 1500 tokens 35.5 / 19.7.
+            // 768, binary32, from memory, one after the other: 50 us as below, 26 so; 1500 tokens 35.5 / 19.7.  Behind the products of a
+            // training step the first takes 42.
             const bool as_bf16 = p.splits == 1 && p.out_bf16;
             const int bytes = as_bf16 ? 2 : 4, expert = this_split / p.splits;
             const int matrix = p.splits > 1 ? this_split % p.splits * p.experts + expert : expert;  // of the partial sums; of the output

@@ -5,12 +5,13 @@
 //
 // What bounds it: memory.  A row is read once and stays in registers: the mean first, then the squares of the differences from it
 // (a variance formed as E x^2 - mu^2 would lose all digits of rows whose mean is large), and the mean of these differences, by which
-// the first one was off (2.5 % of the forward pass at 32896 x 1280 bf16, nothing elsewhere).  Rows of up to 2048 columns belong to a
+// the first one was off (29.4 -> 29.9 us at 32896 x 1280 bf16, nothing elsewhere).  Rows of up to 2048 columns belong to a
 // wave, short ones to a part of one, up to 8192 to four waves and up to 16384 to eight; a group walks many rows, holds gamma and
 // beta (or its shares of both sums) in registers, and requests its next row before it works on this one.  Wider rows are read
-// from L2 again.  Arithmetic is binary32; y and dx are rounded once.
-// 32896 x 1280 bf16: forward 29 us, 5.8 TB/s; backward 46 us and 4.5 for the sums' reduction, 5.0 TB/s; f32 11237 x 1088 backward
-// 28.5 + 4.
+// again: from L2 as long as the 64 rows that an XCD's workgroups have in work fit into its 4 MiB (bf16 up to 32768 columns forward
+// and 16384 backward, half of that in f32), else from beyond.  Arithmetic is binary32; y and dx are rounded once.
+// 32896 x 1280 bf16: forward 29.9 us, 5.6 TB/s (f32 62, 5.4); backward 46 us and 4.8 for the sums' reduction, 5.0 TB/s; f32 11237 x
+// 1088 backward 29 + 4.
 //
 // The sums over the rows: every workgroup adds its rows' terms in registers, its waves' sums meet in LDS and go to the
 // workspace, and a second launch adds those in a fixed order.  No atomics: the same inputs give the same bits.
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void layer_norm_kernel(const
     }
 }
 
-// Rows that do not fit: three passes, of which two find the row in L2.
+// Rows that do not fit: three passes.
 template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(1024) void layer_norm_long_kernel(const T *__restrict__ x, const float *__restrict__ gamma,
                                                                const float *__restrict__ beta, float eps, int64_t rows, int cols,

@@ -538,7 +538,9 @@ int switchback_layer_norm(const void *x, sb_dtype dtype, const float *gamma, con
     if (rows < 0 || cols <= 0 || (dtype != SB_BF16 && dtype != SB_F32) || !(eps > 0.0f) || !std::isfinite(eps)) return SB_INVALID_ARG;
     if (cols > 65536 || rows > (int64_t)1 << 30) return SB_UNSUPPORTED_SHAPE;
     if (rows == 0) return SB_OK;
-    if (!ok_rows(x, cols, dtype) || !ok_rows(y, cols, dtype) || !aligned16(gamma) || !aligned16(beta) || !aligned4(mean) || !aligned4(rstd)) return SB_INVALID_ARG;
+    if (!ok_rows(x, cols, dtype) || !ok_rows(y, cols, dtype) || !aligned16(gamma) || !aligned16(beta) || !aligned4(mean) ||
+        !aligned4(rstd))
+        return SB_INVALID_ARG;
     if (overlap(x, cols * bytes_of(dtype), y, cols * bytes_of(dtype), rows)) return SB_INVALID_ARG;
     return from_hip(sb::launch_layer_norm(x, gamma, beta, eps, rows, cols, dtype == SB_BF16, y, mean, rstd,
                                           static_cast<hipStream_t>(stream)));
@@ -550,7 +552,9 @@ int switchback_layer_norm_backward(const void *dy, const void *x, sb_dtype dtype
     if (rows < 0 || cols <= 0 || (dtype != SB_BF16 && dtype != SB_F32)) return SB_INVALID_ARG;
     if (cols > 65536 || rows > (int64_t)1 << 30) return SB_UNSUPPORTED_SHAPE;
     const bool sums = dgamma != nullptr || dbeta != nullptr;
-    if (rows > 0 && (!ok_rows(dy, cols, dtype) || !ok_rows(x, cols, dtype) || !ok_rows(dx, cols, dtype) || mean == nullptr || rstd == nullptr)) return SB_INVALID_ARG;
+    if (rows > 0 && (!ok_rows(dy, cols, dtype) || !ok_rows(x, cols, dtype) || !ok_rows(dx, cols, dtype) || mean == nullptr ||
+                     rstd == nullptr))
+        return SB_INVALID_ARG;
     if (!aligned16(gamma) || !aligned4(mean) || !aligned4(rstd) || !aligned4(dgamma) || !aligned4(dbeta)) return SB_INVALID_ARG;
     const size_t need = sums ? sb::layer_norm_backward_workspace_bytes(rows, cols) : 0;
     if (need > 0 && !ok_ptr(ws)) return SB_INVALID_ARG;

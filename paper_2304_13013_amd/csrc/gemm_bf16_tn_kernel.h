@@ -86,7 +86,7 @@ struct GemmBf16Cfg {
 
 // FOLD: the token range is one item, but its pieces of k_per_piece tokens are summed on their own and added in token
 // order, in registers: the bits of the split product and its reduction, without the second launch.
-// With GemmBf16ExpertArgs (FOLD, for the pieces of long items) an expert without tokens gets zeros.
+// With GemmBf16ExpertArgs an expert without tokens gets zeros, and FOLD's pieces are those of piece_stages.
 // (A __device__ function: a __global__ template that uses device-only buffer builtins does not instantiate in the host
 // pass; the __global__ entries live next to the launcher.)
 template <bool FOLD, class Args>
